@@ -416,6 +416,63 @@ int pbdr_preprocess_bwd_batch_adam(const pbdr_scene* scene, int32_t num_views, c
                                    const pbdr_splat_grads* g_splats, pbdr_scene_grads* exp_avg, pbdr_scene_grads* exp_avg_sq,
                                    const float lr[5], const pbdr_adam_config* cfg, void* hip_stream);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * Between backward and update (Alg. 1 line 26 names nothing there): the norm of the gradient over all tensors of a
+ * model, its clipping, and the selective Adam step over a list of tensors that takes the clipping factor from the device.
+ *
+ * A list is a HOST array of num_tensors in [0, PBDR_MAX_GRAD_TENSORS] structs; the pointers inside them are device
+ * pointers. A tensor is [planes][n] without gaps; n or planes may be 0 (its pointers are then not looked at). An entry is
+ * USED if visible is NULL or visible[i] != 0 for its point i; entries that are not used are neither counted nor written,
+ * whatever they hold. Gradients of other learned things may be in the same list (planes = 1, visible = NULL), in 16 bits
+ * too.
+ *
+ * pbdr_grad_norm writes result (device, float [2 + num_tensors]):
+ *   result[0]     = norm  = sqrt(sum of g^2 over the used entries of all tensors)
+ *   result[1]     = scale = max_norm / norm where norm > max_norm, else 1; 0 where a used entry is infinite or NaN
+ *   result[2 + t] = norm of tensor t alone
+ * Sums are held in 64 bits (no square of a finite gradient overflows or vanishes) and added in a fixed order: the same
+ * bits on every run, and rounded to 32 bits once (a norm beyond their range is infinite there; scale is right all the
+ * same). max_norm >= 0, infinity included (then scale is 1 or 0).
+ *
+ * pbdr_grad_clip = pbdr_grad_norm, then out = scale * g for the used entries (g where scale is 1; 0 where scale is 0,
+ * even for infinities and NaN), computed in 32 bits and rounded to the tensor's type. out == NULL: in place.
+ *
+ * pbdr_adam_selective_list = pbdr_adam_selective on every tensor of the list with the gradient result[1] * grad (rounded
+ * to 32 bits; 0 where result[1] is 0), bit for bit what pbdr_grad_clip and those calls leave, without the clipped
+ * gradient going through memory. result: what pbdr_grad_norm wrote, or NULL: no clipping. visible == NULL: every point.
+ * cfg->lr is not used, each tensor has its own. cfg->zero_grad clears the used entries of grad.
+ *
+ * What a call writes must not overlap anything else that it reads or writes (a tensor twice in a list that is clipped or
+ * updated, out that covers part of data): PBDR_ERR_INVALID_ARG. Only out == data is allowed.
+ * Workspace: pbdr_grad_workspace_bytes, 256-byte aligned; it need not be cleared, and keeps nothing between calls. */
+#define PBDR_MAX_GRAD_TENSORS 1024
+typedef enum pbdr_dtype { PBDR_F32 = 0, PBDR_F16 = 1, PBDR_BF16 = 2 } pbdr_dtype;
+
+typedef struct pbdr_grad_tensor {
+    void* data;             /* [planes][n] of dtype; only pbdr_grad_clip writes to it, with out == NULL */
+    void* out;              /* pbdr_grad_clip: where the clipped values go, or NULL: to data */
+    const uint8_t* visible; /* [n] or NULL */
+    int64_t n;              /* planes * n at most 2^40 */
+    int32_t planes;
+    int32_t dtype;          /* pbdr_dtype */
+} pbdr_grad_tensor;
+
+typedef struct pbdr_adam_tensor {
+    float *param, *grad, *exp_avg, *exp_avg_sq; /* [planes][n] */
+    const uint8_t* visible;                     /* [n] or NULL */
+    int64_t n;
+    int32_t planes;
+    float lr;
+} pbdr_adam_tensor;
+
+int pbdr_grad_workspace_bytes(int32_t num_tensors, size_t* out_bytes);
+int pbdr_grad_norm(int32_t num_tensors, const pbdr_grad_tensor* tensors, float max_norm, float* result, void* workspace,
+                   size_t workspace_bytes, void* hip_stream);
+int pbdr_grad_clip(int32_t num_tensors, const pbdr_grad_tensor* tensors, float max_norm, float* result, void* workspace,
+                   size_t workspace_bytes, void* hip_stream);
+int pbdr_adam_selective_list(int32_t num_tensors, const pbdr_adam_tensor* tensors, const float* result,
+                             const pbdr_adam_config* cfg, void* hip_stream);
+
 /* Optional per-kernel timing for benchmarks, with HIP events recorded on the stream each kernel is launched on.
  * kernel_mask: bit i enables kernel id i (ids 0 .. pbdr_profile_kernel_count()-1, names from
  * pbdr_profile_kernel_name). At most max_records launches are timed between begin/reset and collect.

@@ -379,3 +379,33 @@ def adam_selective(param, grad, exp_avg, exp_avg_sq, visible, lr, beta1, beta2, 
         v_hat = v[i] / (1.0 - beta2 ** step)
         p[i] = p[i] - lr * m_hat / (np.sqrt(v_hat) + eps)
     return p, m, v
+
+
+# The gradient between backward and update. An entry counts if its point is used (visible None: every point); rows of a tensor
+# [n, ...] are points. fp64; exponents are split off first, so that no square leaves the range.
+def grad_norm(tensors, visibles, max_norm):
+    """(norm over all tensors, factor, [norm of each]). The factor is max_norm / norm where norm > max_norm, 1 elsewhere, 0
+    where the norm is not finite."""
+    each = []
+    for t, vis in zip(tensors, visibles):
+        x = np.asarray(t, dtype=np.float64)
+        x = (x if vis is None else x[np.asarray(vis) != 0]).ravel()
+        top = float(np.abs(x).max()) if x.size else 0.0
+        each.append(top if top == 0.0 or not np.isfinite(top) else top * float(np.sqrt(((x / top) ** 2).sum())))
+    if not np.isfinite(each).all():
+        return (float("nan") if np.isnan(each).any() else float("inf")), 0.0, each
+    top = max(each, default=0.0)
+    norm = top * float(np.sqrt(sum((e / top) ** 2 for e in each))) if top else 0.0
+    return norm, (max_norm / norm if norm > max_norm else 1.0), each
+
+
+def grad_clip(tensor, visible, factor, before):
+    """factor * tensor on the used rows (zero, whatever they hold, for a factor of zero), `before` on the others."""
+    x = np.asarray(tensor, dtype=np.float64)
+    new = np.zeros_like(x) if factor == 0.0 else x * factor
+    if visible is None:
+        return new
+    out = np.array(before, dtype=np.float64)
+    used = np.asarray(visible) != 0
+    out[used] = new[used]
+    return out

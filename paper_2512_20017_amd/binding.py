@@ -26,6 +26,7 @@ PBDR_STATIC_MAX_POINTS = 16384
 PBDR_STATIC_MAX_SIDE = 512
 PBDR_STATIC_MAX_PAIRS = 262144
 PBDR_STATIC_SCRATCH_BYTES = 24 << 20
+PBDR_MAX_GRAD_TENSORS = 1024
 
 EXPORTS = ("pbdr_workspace_bytes", "pbdr_preprocess", "pbdr_bin_sort", "pbdr_render_fwd", "pbdr_render_bwd",
            "pbdr_preprocess_bwd", "pbdr_lists_view", "pbdr_query_lists", "pbdr_status_string", "pbdr_last_hip_error",
@@ -37,7 +38,7 @@ EXPORTS = ("pbdr_workspace_bytes", "pbdr_preprocess", "pbdr_bin_sort", "pbdr_ren
            "pbdr2d_preprocess_patch", "pbdr2d_render_fwd_patch", "pbdr2d_render_bwd_patch",
            "pbdr_l1_loss", "pbdr_mark_visible", "pbdr_adam_selective", "pbdr_preprocess_batch", "pbdr_preprocess_bwd_batch",
            "pbdr_preprocess_bwd_batch_adam", "pbdr_tile_order_view", "pbdr_render_fwd_static", "pbdr_workspace_init",
-           "pbdr_status_view")
+           "pbdr_status_view", "pbdr_grad_workspace_bytes", "pbdr_grad_norm", "pbdr_grad_clip", "pbdr_adam_selective_list")
 
 _f = C.POINTER(C.c_float)
 
@@ -61,6 +62,16 @@ class CPatch(C.Structure):
 class CAdamConfig(C.Structure):
     _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float), ("step", C.c_int32),
                 ("zero_grad", C.c_int32)]
+
+
+class CGradTensor(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("out", C.c_void_p), ("visible", C.c_void_p), ("n", C.c_int64), ("planes", C.c_int32),
+                ("dtype", C.c_int32)]
+
+
+class CAdamTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("exp_avg", C.c_void_p), ("exp_avg_sq", C.c_void_p),
+                ("visible", C.c_void_p), ("n", C.c_int64), ("planes", C.c_int32), ("lr", C.c_float)]
 
 
 class CSplats(C.Structure):
@@ -408,6 +419,171 @@ def pbdr_adam_selective(param, grad, exp_avg, exp_avg_sq, visible, lr, beta1, be
     cfg = CAdamConfig(float(lr), float(beta1), float(beta2), float(eps), int(step), int(bool(zero_grad)))
     _check(lib().pbdr_adam_selective(C.c_int32(n), C.c_int32(planes), _dev(param), _dev(grad), _dev(exp_avg), _dev(exp_avg_sq),
                                      _dev(visible), C.byref(cfg), _stream(stream)))
+
+
+_GRAD_DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+class _TensorList:
+    """Tensors of one device as an array of C structs. The list holds the tensors themselves; before each call it looks whether
+    one has got other memory or another length since (`t.data = ...`, `t.resize_(...)`), and then describes them again."""
+
+    def __init__(self, columns, visible):
+        count = len(columns[0])
+        if any(len(c) != count for c in columns):
+            raise ValueError("pbdr: the lists of tensors differ in length")
+        if visible is None or isinstance(visible, torch.Tensor):
+            visible = [visible] * count
+        elif len(visible) != count:
+            raise ValueError("pbdr: one mask for all tensors, or one (or None) for each")
+        self._columns = [list(c) for c in columns]
+        self._visible = list(visible)
+        self._all = [t for c in (*self._columns, self._visible) for t in c if t is not None]
+        self._describe()
+
+    def __len__(self):
+        return len(self._columns[0])
+
+    def _describe(self):
+        self.device = self._all[0].device if self._all else None
+        for t in self._all:
+            if t.device != self.device:
+                raise ValueError(f"pbdr: tensors of one list lie on {self.device} and {t.device}")
+            if not t.is_contiguous():
+                raise ValueError(f"pbdr: a tensor of shape {tuple(t.shape)} and strides {t.stride()} is not contiguous")
+        sizes = []
+        for ts in zip(*self._columns, self._visible):
+            t, v = ts[0], ts[-1]
+            for x in ts[1:-1]:
+                if x is not None and (x.shape != t.shape or x.dtype != t.dtype):
+                    raise ValueError(f"pbdr: {tuple(x.shape)} {x.dtype} does not go with {tuple(t.shape)} {t.dtype}")
+            if v is None:
+                sizes.append((t.numel(), 1))
+                continue
+            if v.dtype not in (torch.uint8, torch.bool) or t.dim() == 0 or v.shape != t.shape[-1:]:
+                raise ValueError(f"pbdr: a mask of {tuple(v.shape)} {v.dtype} for a tensor of {tuple(t.shape)}: uint8 or bool, one per point")
+            n = t.shape[-1]
+            sizes.append((n, t.numel() // n if n else 0))
+        self._array = self._structs(sizes)
+        self._at = [(t.data_ptr(), t.numel()) for t in self._all]
+
+    def array(self):
+        if [(t.data_ptr(), t.numel()) for t in self._all] != self._at:
+            self._describe()
+        return self._array
+
+
+class GradList(_TensorList):
+    """Gradients whose norm is one number: contiguous float32, float16 or bfloat16 tensors of one device, [..., n].
+    visible: None, or a uint8 / bool mask [n] for all, or a sequence with a mask or None for each tensor.
+    out: where pbdr_grad_clip puts the clipped gradients (same shapes and types), None: in place."""
+
+    def __init__(self, tensors, visible=None, out=None):
+        tensors = list(tensors)
+        super().__init__([tensors, [None] * len(tensors) if out is None else list(out)], visible)
+
+    def _structs(self, sizes):
+        tensors, outs = self._columns
+        for t in tensors:
+            if t.dtype not in _GRAD_DTYPES:
+                raise ValueError(f"pbdr: gradients are float32, float16 or bfloat16, not {t.dtype}")
+        return (CGradTensor * len(tensors))(*[CGradTensor(t.data_ptr(), None if o is None else o.data_ptr(), None if v is None else v.data_ptr(),
+                                                          n, planes, _GRAD_DTYPES[t.dtype])
+                                              for t, o, v, (n, planes) in zip(tensors, outs, self._visible, sizes)])
+
+
+class AdamList(_TensorList):
+    """Parameters with their gradients, both Adam moments and a learning rate each: contiguous float32 tensors of one device.
+    visible as in GradList. set_lrs() changes the learning rates between steps."""
+
+    def __init__(self, params, grads, exp_avg, exp_avg_sq, lrs, visible=None):
+        self._lrs = [float(x) for x in lrs]
+        columns = [list(c) for c in (params, grads, exp_avg, exp_avg_sq)]
+        if len(self._lrs) != len(columns[0]):
+            raise ValueError("pbdr: one learning rate for each tensor")
+        super().__init__(columns, visible)
+
+    def set_lrs(self, lrs):
+        lrs = [float(x) for x in lrs]
+        if len(lrs) != len(self):
+            raise ValueError("pbdr: one learning rate for each tensor")
+        self._lrs = lrs
+        for c, lr in zip(self._array, lrs):
+            c.lr = lr
+
+    def _structs(self, sizes):
+        for t in self._columns[0]:
+            if t.dtype != torch.float32:
+                raise ValueError(f"pbdr: parameters are float32, not {t.dtype}")
+        return (CAdamTensor * len(sizes))(*[CAdamTensor(*[t.data_ptr() for t in ts], None if v is None else v.data_ptr(), n, planes, lr)
+                                            for *ts, v, lr, (n, planes) in zip(*self._columns, self._visible, self._lrs, sizes)])
+
+
+def _on_device(device, stream, call) -> None:
+    """call(stream handle) with the tensors' device current; stream None: that device's current stream."""
+    if device is None or device.type != "cuda":
+        raise ValueError(f"pbdr: tensors lie on {device}, not on a GPU")
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    elif stream.device != device:
+        raise ValueError(f"pbdr: a stream of {stream.device} for tensors on {device}")
+    if device.index == torch.cuda.current_device():
+        _check(call(C.c_void_p(stream.cuda_stream)))
+    else:
+        with torch.cuda.device(device):
+            _check(call(C.c_void_p(stream.cuda_stream)))
+
+
+def _check_result(result, count, device):
+    if result.dtype != torch.float32 or not result.is_contiguous() or result.numel() < 2 + count:
+        raise ValueError(f"pbdr: the result of {count} tensors is a contiguous float32 tensor of {2 + count} values or more")
+    if device is not None and result.device != device:
+        raise ValueError(f"pbdr: the result lies on {result.device}, the tensors on {device}")
+
+
+def pbdr_grad_workspace_bytes(num_tensors: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().pbdr_grad_workspace_bytes(C.c_int32(num_tensors), C.byref(out)))
+    return int(out.value)
+
+
+def alloc_grad_workspace(num_tensors: int, device="cuda") -> torch.Tensor:
+    nbytes = pbdr_grad_workspace_bytes(num_tensors)
+    ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
+    off = (-ws.data_ptr()) % 256
+    return ws[off:off + nbytes]
+
+
+def _grad_call(entry, grads: GradList, max_norm, result, ws, stream) -> None:
+    array, count = grads.array(), len(grads)
+    _check_result(result, count, grads.device)
+    if ws.device != result.device:
+        raise ValueError(f"pbdr: the workspace lies on {ws.device}, the result on {result.device}")
+    _on_device(result.device, stream, lambda s: entry(C.c_int32(count), array, C.c_float(max_norm), C.c_void_p(result.data_ptr()),
+                                                      C.c_void_p(ws.data_ptr()), C.c_size_t(ws.numel()), s))
+
+
+def pbdr_grad_norm(grads: GradList, max_norm: float, result: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    """result (float32 [2 + tensors], device) = {norm over all used entries, clipping factor, norm of each tensor}."""
+    _grad_call(lib().pbdr_grad_norm, grads, max_norm, result, ws, stream)
+
+
+def pbdr_grad_clip(grads: GradList, max_norm: float, result: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    """pbdr_grad_norm, then the used entries times the factor, in place or into the list's `out`."""
+    _grad_call(lib().pbdr_grad_clip, grads, max_norm, result, ws, stream)
+
+
+def pbdr_adam_selective_list(adam: AdamList, beta1, beta2, eps, step, clip: torch.Tensor = None, zero_grad=False, stream=None) -> None:
+    """pbdr_adam_selective on every tensor of the list in one launch; clip: the result of pbdr_grad_norm, whose factor the
+    gradients are taken times, None: as they are."""
+    array, count = adam.array(), len(adam)
+    if count == 0:
+        return
+    if clip is not None:
+        _check_result(clip, 0, adam.device)
+    cfg = CAdamConfig(0.0, float(beta1), float(beta2), float(eps), int(step), int(bool(zero_grad)))
+    _on_device(adam.device, stream, lambda s: lib().pbdr_adam_selective_list(
+        C.c_int32(count), array, C.c_void_p(None if clip is None else clip.data_ptr()), C.byref(cfg), s))
 
 
 def _patch(patch) -> CPatch:

@@ -2,7 +2,9 @@
 #include "../../include/pbdr.h"
 #include "pbdr_internal.h"
 #include "pair_reduce.h"
+#include "grad_ops.h"
 
+#include <algorithm>
 #include <cmath>
 #include <mutex>
 
@@ -215,6 +217,66 @@ static int workspace_ok(void* ws, size_t bytes, int n, int W, int H, uint64_t ca
     if (ws == nullptr || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return PBDR_ERR_INVALID_ARG;
     if (bytes < L->total) return PBDR_ERR_WORKSPACE_TOO_SMALL;
     return PBDR_OK;
+}
+
+// Memory that a call touches, to see that what it writes overlaps nothing else. Ranges lie on the caller's stack.
+struct Range {
+    uintptr_t from, to;
+    bool written;
+};
+static bool overlap(Range* r, int count)
+{
+    std::sort(r, r + count, [](const Range& a, const Range& b) { return a.from < b.from; });
+    uintptr_t any = 0, written = 0;      // where the ranges so far end
+    for (int i = 0; i < count; ++i) {
+        if (r[i].from == r[i].to) continue;
+        if (r[i].from < written || (r[i].written && r[i].from < any)) return true;
+        any = std::max(any, r[i].to);
+        if (r[i].written) written = std::max(written, r[i].to);
+    }
+    return false;
+}
+static Range range(const void* p, uint64_t bytes, bool written)
+{
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    return Range{a, a + bytes, written};
+}
+
+static_assert(PBDR_MAX_GRAD_TENSORS == kGradMaxTensors && PBDR_F32 == kGradF32 && PBDR_F16 == kGradF16 && PBDR_BF16 == kGradBF16, "");
+
+constexpr int64_t kMaxEntries = (int64_t)1 << 40;      // of a tensor: units of its work are numbered in 32 bits
+static bool check_extent(int64_t n, int32_t planes)
+{
+    return n >= 0 && planes >= 0 && n <= kMaxEntries && (planes == 0 || n <= kMaxEntries / planes);
+}
+
+// The list as the kernels see it; clip: outputs too, which overlap nothing.
+static bool to_dev(int32_t count, const pbdr_grad_tensor* list, bool clip, const float* result, const void* workspace, GradTensorDev* out)
+{
+    if (count < 0 || count > kGradMaxTensors || (count > 0 && list == nullptr)) return false;
+    Range r[3 * kGradMaxTensors + 2];
+    int nr = 0;
+    r[nr++] = range(result, (2 + (uint64_t)count) * sizeof(float), true);
+    r[nr++] = range(workspace, kGradWorkspace, true);
+    for (int i = 0; i < count; ++i) {
+        const pbdr_grad_tensor& t = list[i];
+        if (!check_extent(t.n, t.planes) || t.dtype < PBDR_F32 || t.dtype > PBDR_BF16) return false;
+        GradTensorDev& d = out[i];
+        d = GradTensorDev{t.data, t.out ? t.out : t.data, t.visible, (uint64_t)t.n, (uint64_t)t.n * (uint64_t)t.planes, (uint32_t)t.planes, 0u, t.dtype};
+        if (d.count == 0) continue;
+        if (!aligned16(t.data) || (t.visible && !aligned16(t.visible)) || (clip && !aligned16(d.out))) return false;
+        const uint64_t bytes = d.count * (t.dtype == PBDR_F32 ? 4 : 2);
+        r[nr++] = range(t.data, bytes, clip && d.out == t.data);
+        if (clip && d.out != t.data) r[nr++] = range(d.out, bytes, true);
+        if (t.visible) r[nr++] = range(t.visible, d.n, false);
+    }
+    return !overlap(r, nr);
+}
+
+static int grad_workspace_ok(const void* workspace, size_t bytes)
+{
+    if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return PBDR_ERR_INVALID_ARG;
+    return bytes < kGradWorkspace ? PBDR_ERR_WORKSPACE_TOO_SMALL : PBDR_OK;
 }
 
 }  // namespace pbdr
@@ -759,6 +821,70 @@ int pbdr_preprocess_bwd_batch_adam(const pbdr_scene* scene, int32_t num_views, c
     opt.m_mean = m.mean; opt.m_log_scale = m.log_scale; opt.m_quat = m.quat; opt.m_logit = m.logit; opt.m_sh = m.sh;
     opt.v_mean = v2.mean; opt.v_log_scale = v2.log_scale; opt.v_quat = v2.quat; opt.v_logit = v2.logit; opt.v_sh = v2.sh;
     return hip_result(launch_preprocess_bwd_batch_adam(dev(scene), bc, bg, opt, (hipStream_t)hip_stream));
+}
+
+int pbdr_grad_workspace_bytes(int32_t num_tensors, size_t* out_bytes)
+{
+    if (num_tensors < 0 || num_tensors > PBDR_MAX_GRAD_TENSORS || !out_bytes) return PBDR_ERR_INVALID_ARG;
+    *out_bytes = align256(kGradWorkspace);
+    return PBDR_OK;
+}
+
+static int grad_impl(int32_t num_tensors, const pbdr_grad_tensor* tensors, float max_norm, float* result, void* workspace,
+                     size_t workspace_bytes, bool clip, void* hip_stream)
+{
+    if (!(max_norm >= 0.f) || !aligned16(result)) return PBDR_ERR_INVALID_ARG;
+    const int st = grad_workspace_ok(workspace, workspace_bytes);
+    if (st != PBDR_OK) return st;
+    GradTensorDev list[kGradMaxTensors];
+    if (!to_dev(num_tensors, tensors, clip, result, workspace, list)) return PBDR_ERR_INVALID_ARG;
+    hipError_t e = launch_grad_norm(num_tensors, list, max_norm, result, (char*)workspace, (hipStream_t)hip_stream);
+    if (e == hipSuccess && clip) e = launch_grad_scale(num_tensors, list, result, (hipStream_t)hip_stream);
+    return hip_result(e);
+}
+
+int pbdr_grad_norm(int32_t num_tensors, const pbdr_grad_tensor* tensors, float max_norm, float* result, void* workspace,
+                   size_t workspace_bytes, void* hip_stream)
+{
+    return grad_impl(num_tensors, tensors, max_norm, result, workspace, workspace_bytes, false, hip_stream);
+}
+
+int pbdr_grad_clip(int32_t num_tensors, const pbdr_grad_tensor* tensors, float max_norm, float* result, void* workspace,
+                   size_t workspace_bytes, void* hip_stream)
+{
+    return grad_impl(num_tensors, tensors, max_norm, result, workspace, workspace_bytes, true, hip_stream);
+}
+
+int pbdr_adam_selective_list(int32_t num_tensors, const pbdr_adam_tensor* tensors, const float* result,
+                             const pbdr_adam_config* cfg, void* hip_stream)
+{
+    if (num_tensors < 0 || num_tensors > PBDR_MAX_GRAD_TENSORS || (num_tensors > 0 && !tensors) || !cfg || (result && !aligned16(result)))
+        return PBDR_ERR_INVALID_ARG;
+    if (!(cfg->beta1 >= 0.f && cfg->beta1 < 1.f) || !(cfg->beta2 >= 0.f && cfg->beta2 < 1.f) || !(cfg->eps > 0.f) || cfg->step < 1)
+        return PBDR_ERR_INVALID_ARG;
+    AdamTensorDev list[kGradMaxTensors];
+    Range r[5 * kGradMaxTensors + 1];
+    int nr = 0;
+    if (result) r[nr++] = range(result, 2 * sizeof(float), false);
+    for (int i = 0; i < num_tensors; ++i) {
+        const pbdr_adam_tensor& t = tensors[i];
+        if (!check_extent(t.n, t.planes) || !(t.lr >= 0.f)) return PBDR_ERR_INVALID_ARG;
+        const AdamDev a = make_adam(t.lr, cfg->beta1, cfg->beta2, cfg->eps, cfg->step, cfg->zero_grad);
+        list[i] = AdamTensorDev{t.param, t.grad, t.exp_avg, t.exp_avg_sq, t.visible, (uint64_t)t.n, (uint64_t)t.n * (uint64_t)t.planes,
+                                (uint32_t)t.planes, 0u, a.step_size};
+        const uint64_t bytes = list[i].count * sizeof(float);
+        if (bytes == 0) continue;
+        if (!aligned16(t.param) || !aligned16(t.grad) || !aligned16(t.exp_avg) || !aligned16(t.exp_avg_sq) || (t.visible && !aligned16(t.visible)))
+            return PBDR_ERR_INVALID_ARG;
+        r[nr++] = range(t.param, bytes, true);
+        r[nr++] = range(t.grad, bytes, cfg->zero_grad != 0);
+        r[nr++] = range(t.exp_avg, bytes, true);
+        r[nr++] = range(t.exp_avg_sq, bytes, true);
+        if (t.visible) r[nr++] = range(t.visible, list[i].n, false);
+    }
+    if (overlap(r, nr)) return PBDR_ERR_INVALID_ARG;
+    return hip_result(launch_adam_list(num_tensors, list, make_adam(0.f, cfg->beta1, cfg->beta2, cfg->eps, cfg->step, cfg->zero_grad), result,
+                                       (hipStream_t)hip_stream));
 }
 
 int pbdr_query_lists(void* workspace, size_t workspace_bytes, int32_t n, int32_t width, int32_t height,

@@ -7,7 +7,8 @@ namespace pbdr {
 
 enum KernelId {
     kKPreprocess = 0, kKCountVisible, kKTileCount, kKTileLists, kKPack, kKFill,
-    kKCompositeFwd, kKCompositeBwd, kKPreprocessBwd, kKStats, kKGather, kKGroupCull, kKLoss, kKAdam, kKTileDepthSort, kKernelCount
+    kKCompositeFwd, kKCompositeBwd, kKPreprocessBwd, kKStats, kKGather, kKGroupCull, kKLoss, kKAdam, kKTileDepthSort,
+    kKGradNorm, kKGradScale, kKAdamList, kKernelCount
 };
 
 struct ProfState {
