@@ -10,7 +10,7 @@
 //
 // A tensor is cut into units. Without a mask it is one row of planes * n values, and a unit is kDenseVecs vectors of 16 bytes per
 // lane. With a mask a unit is one vector of points per lane and up to kMaskPlanes planes: the mask is read once for all of them,
-// and a lane that has no used point reads nothing else.
+// and a lane that has no used point reads nothing else. A lane that has one reads whole vectors, all planes of the unit at once.
 #include "grad_ops.h"
 
 #include <cmath>
@@ -28,23 +28,33 @@ template <class T> struct GradVec {
     typedef T V __attribute__((ext_vector_type(kN), aligned(sizeof(T))));
 };
 
-// the used points among kN consecutive ones: bit k is point at + k
+// the bytes of the mask for kN consecutive points, zero beyond the last point
 template <int kN>
-__device__ __forceinline__ uint32_t used_bits(const uint8_t* __restrict__ visible, uint64_t at, uint64_t n)
+__device__ __forceinline__ uint64_t mask_bytes(const uint8_t* __restrict__ visible, uint64_t at, uint64_t n)
 {
-    uint32_t bits = 0;
-    if (at + kN <= n) {
-#pragma unroll
-        for (int w = 0; w < kN / 4; ++w) {
-            const uint32_t m = *reinterpret_cast<const uint32_t*>(visible + at + 4 * w);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) bits |= ((m >> (8 * k)) & 0xffu) ? 1u << (4 * w + k) : 0u;
-        }
-    } else {
-        for (int k = 0; k < kN; ++k)
-            if (at + k < n && visible[at + k]) bits |= 1u << k;
-    }
-    return bits;
+    if (at + kN <= n) return kN == 4 ? *reinterpret_cast<const uint32_t*>(visible + at) : *reinterpret_cast<const uint64_t*>(visible + at);
+    uint64_t m = 0;
+    for (int k = 0; k < kN; ++k)
+        if (at + k < n) m |= (uint64_t)visible[at + k] << (8 * k);
+    return m;
+}
+template <int kN>
+__device__ __forceinline__ bool used(uint64_t mask, int k)
+{
+    return ((kN == 4 ? (uint32_t)mask >> (8 * k) : (uint32_t)(mask >> (8 * k))) & 0xffu) != 0u;
+}
+
+// a unit of a masked tensor: this lane's points and the planes
+struct MaskedUnit {
+    uint64_t at;
+    uint32_t p0, p1;
+};
+template <int kN, uint32_t kPlanes>
+__device__ __forceinline__ MaskedUnit masked_unit(uint32_t u, uint32_t planes)
+{
+    const uint32_t groups = (planes + kPlanes - 1) / kPlanes;
+    const uint32_t seg = u / groups, p0 = (u - seg * groups) * kPlanes;
+    return MaskedUnit{((uint64_t)seg * kGradBlock + threadIdx.x) * kN, p0, min(p0 + kPlanes, planes)};
 }
 
 template <class T>
@@ -86,24 +96,41 @@ __device__ double sum_squares(const GradTensorDev& t, uint32_t first, uint32_t s
             }
         }
     } else {
-        const uint32_t groups = (t.planes + kMaskPlanes - 1) / kMaskPlanes;
-        for (uint32_t u = first; u < t.units; u += step) {
-            const uint32_t seg = u / groups, p0 = (u - seg * groups) * kMaskPlanes, p1 = min(p0 + kMaskPlanes, t.planes);
-            const uint64_t at = ((uint64_t)seg * kGradBlock + threadIdx.x) * kN;
-            const uint32_t bits = at < t.n ? used_bits<kN>(t.visible, at, t.n) : 0u;
-            if (bits == 0u) continue;
-            const T* row = data + (uint64_t)p0 * t.n + at;
-            if (at + kN <= t.n) {
-                for (uint32_t p = p0; p < p1; ++p, row += t.n) {
-                    const Vec v = *reinterpret_cast<const Vec*>(row);
-#pragma unroll
-                    for (int k = 0; k < kN; ++k) add_square(acc[k & 3], (bits >> k) & 1u ? v[k] : (T)0.f);
-                }
-            } else {
-                for (uint32_t p = p0; p < p1; ++p, row += t.n)
-                    for (int k = 0; k < kN; ++k)
-                        if ((bits >> k) & 1u) add_square(acc[0], row[k]);
+        if (first >= t.units) return 0.;
+        MaskedUnit w = masked_unit<kN, kMaskPlanes>(first, t.planes);
+        uint64_t mask = mask_bytes<kN>(t.visible, w.at, t.n);
+        for (uint32_t u = first;;) {
+            // the next unit's mask is on its way while this unit's values come
+            const bool more = u + step < t.units;
+            MaskedUnit w1 = w;
+            uint64_t mask1 = 0;
+            if (more) {
+                w1 = masked_unit<kN, kMaskPlanes>(u + step, t.planes);
+                mask1 = mask_bytes<kN>(t.visible, w1.at, t.n);
             }
+            if (mask != 0) {
+                const T* row = data + (uint64_t)w.p0 * t.n + w.at;
+                if (w.at + kN <= t.n) {
+                    Vec v[kMaskPlanes];
+#pragma unroll
+                    for (uint32_t j = 0; j < kMaskPlanes; ++j)
+                        if (w.p0 + j < w.p1) v[j] = *reinterpret_cast<const Vec*>(row + (uint64_t)j * t.n);
+#pragma unroll
+                    for (uint32_t j = 0; j < kMaskPlanes; ++j)
+                        if (w.p0 + j < w.p1) {
+#pragma unroll
+                            for (int k = 0; k < kN; ++k) add_square(acc[k & 3], used<kN>(mask, k) ? (T)v[j][k] : (T)0.f);
+                        }
+                } else {
+                    for (uint32_t p = w.p0; p < w.p1; ++p, row += t.n)
+                        for (int k = 0; k < kN; ++k)
+                            if (used<kN>(mask, k)) add_square(acc[0], row[k]);
+                }
+            }
+            if (!more) break;
+            u += step;
+            w = w1;
+            mask = mask1;
         }
     }
     return (acc[0] + acc[1]) + (acc[2] + acc[3]);
@@ -199,27 +226,37 @@ __device__ void write_scaled(const GradTensorDev& t, float scale, uint32_t first
             }
         }
     } else {
-        const uint32_t groups = (t.planes + kMaskPlanes - 1) / kMaskPlanes;
         for (uint32_t u = first; u < t.units; u += step) {
-            const uint32_t seg = u / groups, p0 = (u - seg * groups) * kMaskPlanes, p1 = min(p0 + kMaskPlanes, t.planes);
-            const uint64_t at = ((uint64_t)seg * kGradBlock + threadIdx.x) * kN;
-            const uint32_t bits = at < t.n ? used_bits<kN>(t.visible, at, t.n) : 0u;
-            if (bits == 0u) continue;
-            const uint64_t o = (uint64_t)p0 * t.n + at;
-            if (bits == (1u << kN) - 1u) {
-                for (uint32_t p = p0; p < p1; ++p) {
-                    const uint64_t a = o + (uint64_t)(p - p0) * t.n;
-                    Vec v = *reinterpret_cast<const Vec*>(data + a);
+            const MaskedUnit w = masked_unit<kN, kMaskPlanes>(u, t.planes);
+            const uint64_t mask = mask_bytes<kN>(t.visible, w.at, t.n);
+            if (mask == 0) continue;
+            bool all = true;
 #pragma unroll
-                    for (int k = 0; k < kN; ++k) v[k] = scaled((T)v[k], scale);
-                    *reinterpret_cast<Vec*>(out + a) = v;
-                }
+            for (int k = 0; k < kN; ++k) all = all && used<kN>(mask, k);
+            const uint64_t o = (uint64_t)w.p0 * t.n + w.at;
+            if (w.at + kN <= t.n) {
+                Vec v[kMaskPlanes];
+#pragma unroll
+                for (uint32_t j = 0; j < kMaskPlanes; ++j)
+                    if (w.p0 + j < w.p1) v[j] = *reinterpret_cast<const Vec*>(data + o + (uint64_t)j * t.n);
+#pragma unroll
+                for (uint32_t j = 0; j < kMaskPlanes; ++j)
+                    if (w.p0 + j < w.p1) {
+                        T* to = out + o + (uint64_t)j * t.n;
+#pragma unroll
+                        for (int k = 0; k < kN; ++k) v[j][k] = scaled((T)v[j][k], scale);
+                        if (all) *reinterpret_cast<Vec*>(to) = v[j];
+                        else
+#pragma unroll
+                            for (int k = 0; k < kN; ++k)
+                                if (used<kN>(mask, k)) to[k] = v[j][k];
+                    }
             } else {
-                for (uint32_t p = p0; p < p1; ++p) {
-                    const uint64_t a = o + (uint64_t)(p - p0) * t.n;
-                    for (int k = 0; k < kN; ++k)
-                        if ((bits >> k) & 1u) out[a + k] = scaled(data[a + k], scale);
-                }
+                for (uint32_t p = w.p0; p < w.p1; ++p)
+                    for (int k = 0; k < kN; ++k) {
+                        const uint64_t a = (uint64_t)p * t.n + w.at + k;
+                        if (used<kN>(mask, k)) out[a] = scaled(data[a], scale);
+                    }
             }
         }
     }
@@ -246,22 +283,31 @@ __device__ __forceinline__ void adam_clipped(const AdamDev& c, float scale, floa
     if (c.zero_grad) *g = 0.f;
 }
 
-__device__ __forceinline__ void adam_clipped4(const AdamDev& c, float scale, float* p, float* g, float* m, float* v)
+// four entries, of which those with a zero in the mask get their own bits back
+struct AdamVec {
+    GradVec<float>::V p, g, m, v;
+};
+__device__ __forceinline__ AdamVec adam_load(const AdamTensorDev& t, uint64_t at)
 {
     using Vec = GradVec<float>::V;
-    Vec x = *reinterpret_cast<Vec*>(p);
-    const Vec y = *reinterpret_cast<Vec*>(g);
-    Vec mm = *reinterpret_cast<Vec*>(m), vv = *reinterpret_cast<Vec*>(v);
+    return AdamVec{*reinterpret_cast<const Vec*>(t.param + at), *reinterpret_cast<const Vec*>(t.grad + at), *reinterpret_cast<const Vec*>(t.m + at),
+                   *reinterpret_cast<const Vec*>(t.v + at)};
+}
+__device__ __forceinline__ void adam_store(const AdamDev& c, float scale, uint32_t mask, const AdamTensorDev& t, uint64_t at, AdamVec x)
+{
+    using Vec = GradVec<float>::V;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        float a = x[k], b = mm[k], d = vv[k];
-        adam_one(c, a, scaled((float)y[k], scale), b, d);
-        x[k] = a; mm[k] = b; vv[k] = d;
+        float a = x.p[k], b = x.m[k], d = x.v[k];
+        adam_one(c, a, scaled((float)x.g[k], scale), b, d);
+        if (used<4>(mask, k)) {
+            x.p[k] = a; x.m[k] = b; x.v[k] = d; x.g[k] = 0.f;
+        }
     }
-    *reinterpret_cast<Vec*>(p) = x;
-    *reinterpret_cast<Vec*>(m) = mm;
-    *reinterpret_cast<Vec*>(v) = vv;
-    if (c.zero_grad) *reinterpret_cast<Vec*>(g) = (Vec)0.f;
+    *reinterpret_cast<Vec*>(t.param + at) = x.p;
+    *reinterpret_cast<Vec*>(t.m + at) = x.m;
+    *reinterpret_cast<Vec*>(t.v + at) = x.v;
+    if (c.zero_grad) *reinterpret_cast<Vec*>(t.grad + at) = x.g;
 }
 
 __global__ __launch_bounds__(kGradBlock) void k_adam_list(AdamTable tab, const float* __restrict__ result)
@@ -284,24 +330,29 @@ __global__ __launch_bounds__(kGradBlock) void k_adam_list(AdamTable tab, const f
 #pragma unroll
             for (int j = 0; j < kAdamVecs; ++j) {
                 const uint64_t at = base + (uint64_t)j * kGradBlock * 4;
-                if (at + 4 <= t.count) adam_clipped4(c, scale, t.param + at, t.grad + at, t.m + at, t.v + at);
+                if (at + 4 <= t.count) adam_store(c, scale, ~0u, t, at, adam_load(t, at));
                 else
                     for (uint64_t i = at; i < t.count; ++i) adam_clipped(c, scale, t.param + i, t.grad + i, t.m + i, t.v + i);
             }
         }
     } else {
-        const uint32_t groups = (t.planes + kMaskPlanes - 1) / kMaskPlanes;
         for (uint32_t u = first; u < t.units; u += step) {
-            const uint32_t seg = u / groups, p0 = (u - seg * groups) * kMaskPlanes, p1 = min(p0 + kMaskPlanes, t.planes);
-            const uint64_t at = ((uint64_t)seg * kGradBlock + threadIdx.x) * 4;
-            const uint32_t bits = at < t.n ? used_bits<4>(t.visible, at, t.n) : 0u;
-            if (bits == 0u) continue;
-            for (uint32_t p = p0; p < p1; ++p) {
-                const uint64_t a = (uint64_t)p * t.n + at;
-                if (bits == 15u) adam_clipped4(c, scale, t.param + a, t.grad + a, t.m + a, t.v + a);
-                else
+            const MaskedUnit w = masked_unit<4, kAdamPlanes>(u, t.planes);
+            const uint32_t mask = (uint32_t)mask_bytes<4>(t.visible, w.at, t.n);
+            if (mask == 0) continue;
+            uint64_t at = (uint64_t)w.p0 * t.n + w.at;
+            if (w.at + 4 <= t.n) {
+                AdamVec x[kAdamPlanes];
+#pragma unroll
+                for (uint32_t j = 0; j < kAdamPlanes; ++j)
+                    if (w.p0 + j < w.p1) x[j] = adam_load(t, at + j * t.n);
+#pragma unroll
+                for (uint32_t j = 0; j < kAdamPlanes; ++j)
+                    if (w.p0 + j < w.p1) adam_store(c, scale, mask, t, at + j * t.n, x[j]);
+            } else {
+                for (uint32_t p = w.p0; p < w.p1; ++p, at += t.n)
                     for (int k = 0; k < 4; ++k)
-                        if ((bits >> k) & 1u) adam_clipped(c, scale, t.param + a + k, t.grad + a + k, t.m + a + k, t.v + a + k);
+                        if (used<4>(mask, k)) adam_clipped(c, scale, t.param + at + k, t.grad + at + k, t.m + at + k, t.v + at + k);
             }
         }
     }
@@ -309,12 +360,12 @@ __global__ __launch_bounds__(kGradBlock) void k_adam_list(AdamTable tab, const f
 
 // Units of a tensor, and how many workgroups share the units of a table: one unit each up to kGradBlocks of them, then equal runs.
 template <class T>
-static void cut_units(T& t, int value_bytes, int dense_vecs)
+static void cut_units(T& t, int value_bytes, int dense_vecs, uint32_t planes)
 {
     const uint64_t vec = 16 / value_bytes;
     if (t.count == 0) t.units = 0;
     else if (t.visible == nullptr) t.units = (uint32_t)((t.count + kGradBlock * vec * dense_vecs - 1) / (kGradBlock * vec * dense_vecs));
-    else t.units = (uint32_t)((t.n + kGradBlock * vec - 1) / (kGradBlock * vec)) * ((t.planes + kMaskPlanes - 1) / kMaskPlanes);
+    else t.units = (uint32_t)((t.n + kGradBlock * vec - 1) / (kGradBlock * vec)) * ((t.planes + planes - 1) / planes);
 }
 
 template <class Table>
@@ -338,7 +389,7 @@ static uint32_t fill_table(GradTable& tab, const GradTensorDev* list, int count)
     tab.count = count;
     for (int i = 0; i < count; ++i) {
         tab.t[i] = list[i];
-        cut_units(tab.t[i], list[i].dtype == kGradF32 ? 4 : 2, kDenseVecs);
+        cut_units(tab.t[i], list[i].dtype == kGradF32 ? 4 : 2, kDenseVecs, kMaskPlanes);
     }
     return cut_blocks(tab, kGradBlocks);
 }
@@ -380,7 +431,7 @@ hipError_t launch_adam_list(int count, const AdamTensorDev* list, const AdamDev&
         tab.count = count - at < kAdamTableTensors ? count - at : kAdamTableTensors;
         for (int i = 0; i < tab.count; ++i) {
             tab.t[i] = list[at + i];
-            cut_units(tab.t[i], 4, kAdamVecs);
+            cut_units(tab.t[i], 4, kAdamVecs, kAdamPlanes);
         }
         const uint32_t blocks = cut_blocks(tab, kAdamBlocks);
         if (blocks) hipLaunchKernelGGL(k_adam_list, dim3(blocks), dim3(kGradBlock), 0, s, tab, result);
