@@ -444,7 +444,8 @@ int pbdr_preprocess_bwd_batch_adam(const pbdr_scene* scene, int32_t num_views, c
  *
  * What a call writes must not overlap anything else that it reads or writes (a tensor twice in a list that is clipped or
  * updated, out that covers part of data): PBDR_ERR_INVALID_ARG. Only out == data is allowed.
- * Workspace: pbdr_grad_workspace_bytes, 256-byte aligned; it need not be cleared, and keeps nothing between calls. */
+ * Workspace: pbdr_grad_workspace_bytes, 256-byte aligned and ZERO-FILLED ONCE before its first use (pbdr_workspace_init):
+ * a counter in it is at zero between calls. It serves lists of any length, one call at a time. */
 #define PBDR_MAX_GRAD_TENSORS 1024
 typedef enum pbdr_dtype { PBDR_F32 = 0, PBDR_F16 = 1, PBDR_BF16 = 2 } pbdr_dtype;
 
@@ -452,7 +453,7 @@ typedef struct pbdr_grad_tensor {
     void* data;             /* [planes][n] of dtype; only pbdr_grad_clip writes to it, with out == NULL */
     void* out;              /* pbdr_grad_clip: where the clipped values go, or NULL: to data */
     const uint8_t* visible; /* [n] or NULL */
-    int64_t n;              /* planes * n at most 2^40 */
+    int64_t n;              /* planes below 2^24, planes * n at most 2^40 */
     int32_t planes;
     int32_t dtype;          /* pbdr_dtype */
 } pbdr_grad_tensor;

@@ -114,6 +114,9 @@ def lib():
         L.pbdr_profile_kernel_name.restype = C.c_char_p
         for name in EXPORTS:
             getattr(L, name)
+        # the calls between backward and update take plain numbers and addresses: their latency counts
+        L.pbdr_grad_norm.argtypes = L.pbdr_grad_clip.argtypes = [C.c_int32, C.c_void_p, C.c_float, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.pbdr_adam_selective_list.argtypes = [C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
         _lib = L
     return _lib
 
@@ -425,8 +428,9 @@ _GRAD_DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
 class _TensorList:
-    """Tensors of one device as an array of C structs. The list holds the tensors themselves; before each call it looks whether
-    one has got other memory or another length since (`t.data = ...`, `t.resize_(...)`), and then describes them again."""
+    """Tensors of one device as an array of C structs. Before each call the list looks whether a tensor has got other memory since
+    (`t.data = ...`), and then describes them again. It holds the tensors and the memory that it has described, so that no other
+    memory comes to lie at the same address."""
 
     def __init__(self, columns, visible):
         count = len(columns[0])
@@ -465,10 +469,11 @@ class _TensorList:
             n = t.shape[-1]
             sizes.append((n, t.numel() // n if n else 0))
         self._array = self._structs(sizes)
-        self._at = [(t.data_ptr(), t.numel()) for t in self._all]
+        self._memory = [t.untyped_storage() for t in self._all]
+        self._at = [t.data_ptr() for t in self._all]
 
     def array(self):
-        if [(t.data_ptr(), t.numel()) for t in self._all] != self._at:
+        if list(map(torch.Tensor.data_ptr, self._all)) != self._at:
             self._describe()
         return self._array
 
@@ -519,26 +524,27 @@ class AdamList(_TensorList):
                                             for *ts, v, lr, (n, planes) in zip(*self._columns, self._visible, self._lrs, sizes)])
 
 
-def _on_device(device, stream, call) -> None:
-    """call(stream handle) with the tensors' device current; stream None: that device's current stream."""
-    if device is None or device.type != "cuda":
+def _call_on(device, stream, entry, *args) -> None:
+    """entry(*args, stream) with the tensors' device current; stream None: that device's current stream."""
+    if device.type != "cuda":
         raise ValueError(f"pbdr: tensors lie on {device}, not on a GPU")
     if stream is None:
         stream = torch.cuda.current_stream(device)
     elif stream.device != device:
         raise ValueError(f"pbdr: a stream of {stream.device} for tensors on {device}")
     if device.index == torch.cuda.current_device():
-        _check(call(C.c_void_p(stream.cuda_stream)))
+        _check(entry(*args, stream.cuda_stream))
     else:
         with torch.cuda.device(device):
-            _check(call(C.c_void_p(stream.cuda_stream)))
+            _check(entry(*args, stream.cuda_stream))
 
 
-def _check_result(result, count, device):
+def _result_address(result, count, device):
     if result.dtype != torch.float32 or not result.is_contiguous() or result.numel() < 2 + count:
         raise ValueError(f"pbdr: the result of {count} tensors is a contiguous float32 tensor of {2 + count} values or more")
     if device is not None and result.device != device:
         raise ValueError(f"pbdr: the result lies on {result.device}, the tensors on {device}")
+    return result.data_ptr()
 
 
 def pbdr_grad_workspace_bytes(num_tensors: int) -> int:
@@ -548,19 +554,17 @@ def pbdr_grad_workspace_bytes(num_tensors: int) -> int:
 
 
 def alloc_grad_workspace(num_tensors: int, device="cuda") -> torch.Tensor:
-    nbytes = pbdr_grad_workspace_bytes(num_tensors)
-    ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
-    off = (-ws.data_ptr()) % 256
-    return ws[off:off + nbytes]
+    with torch.cuda.device(device):
+        return _alloc_ws(pbdr_grad_workspace_bytes(num_tensors), device)
 
 
 def _grad_call(entry, grads: GradList, max_norm, result, ws, stream) -> None:
-    array, count = grads.array(), len(grads)
-    _check_result(result, count, grads.device)
-    if ws.device != result.device:
-        raise ValueError(f"pbdr: the workspace lies on {ws.device}, the result on {result.device}")
-    _on_device(result.device, stream, lambda s: entry(C.c_int32(count), array, C.c_float(max_norm), C.c_void_p(result.data_ptr()),
-                                                      C.c_void_p(ws.data_ptr()), C.c_size_t(ws.numel()), s))
+    array = grads.array()
+    count, device = len(array), result.device
+    to = _result_address(result, count, grads.device)
+    if ws.device != device:
+        raise ValueError(f"pbdr: the workspace lies on {ws.device}, the result on {device}")
+    _call_on(device, stream, entry, count, array, max_norm, to, ws.data_ptr(), ws.numel())
 
 
 def pbdr_grad_norm(grads: GradList, max_norm: float, result: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
@@ -576,14 +580,12 @@ def pbdr_grad_clip(grads: GradList, max_norm: float, result: torch.Tensor, ws: t
 def pbdr_adam_selective_list(adam: AdamList, beta1, beta2, eps, step, clip: torch.Tensor = None, zero_grad=False, stream=None) -> None:
     """pbdr_adam_selective on every tensor of the list in one launch; clip: the result of pbdr_grad_norm, whose factor the
     gradients are taken times, None: as they are."""
-    array, count = adam.array(), len(adam)
-    if count == 0:
+    array = adam.array()
+    if len(array) == 0:
         return
-    if clip is not None:
-        _check_result(clip, 0, adam.device)
+    factor = None if clip is None else _result_address(clip, 0, adam.device)
     cfg = CAdamConfig(0.0, float(beta1), float(beta2), float(eps), int(step), int(bool(zero_grad)))
-    _on_device(adam.device, stream, lambda s: lib().pbdr_adam_selective_list(
-        C.c_int32(count), array, C.c_void_p(None if clip is None else clip.data_ptr()), C.byref(cfg), s))
+    _call_on(adam.device, stream, lib().pbdr_adam_selective_list, len(array), array, factor, C.byref(cfg))
 
 
 def _patch(patch) -> CPatch:

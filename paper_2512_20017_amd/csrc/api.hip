@@ -247,7 +247,7 @@ static_assert(PBDR_MAX_GRAD_TENSORS == kGradMaxTensors && PBDR_F32 == kGradF32 &
 constexpr int64_t kMaxEntries = (int64_t)1 << 40;      // of a tensor: units of its work are numbered in 32 bits
 static bool check_extent(int64_t n, int32_t planes)
 {
-    return n >= 0 && planes >= 0 && n <= kMaxEntries && (planes == 0 || n <= kMaxEntries / planes);
+    return n >= 0 && planes >= 0 && planes < (1 << 24) && n <= kMaxEntries && (planes == 0 || n <= kMaxEntries / planes);
 }
 
 // The list as the kernels see it; clip: outputs too, which overlap nothing.
@@ -257,15 +257,15 @@ static bool to_dev(int32_t count, const pbdr_grad_tensor* list, bool clip, const
     Range r[3 * kGradMaxTensors + 2];
     int nr = 0;
     r[nr++] = range(result, (2 + (uint64_t)count) * sizeof(float), true);
-    r[nr++] = range(workspace, kGradWorkspace, true);
+    r[nr++] = range(workspace, sizeof(GradWorkspace), true);
     for (int i = 0; i < count; ++i) {
         const pbdr_grad_tensor& t = list[i];
         if (!check_extent(t.n, t.planes) || t.dtype < PBDR_F32 || t.dtype > PBDR_BF16) return false;
         GradTensorDev& d = out[i];
-        d = GradTensorDev{t.data, t.out ? t.out : t.data, t.visible, (uint64_t)t.n, (uint64_t)t.n * (uint64_t)t.planes, (uint32_t)t.planes, 0u, t.dtype};
-        if (d.count == 0) continue;
+        d = GradTensorDev{t.data, t.out ? t.out : t.data, t.visible, (uint64_t)t.n, (uint32_t)t.planes, (uint32_t)t.dtype, 0u};
+        if (t.n == 0 || t.planes == 0) continue;
         if (!aligned16(t.data) || (t.visible && !aligned16(t.visible)) || (clip && !aligned16(d.out))) return false;
-        const uint64_t bytes = d.count * (t.dtype == PBDR_F32 ? 4 : 2);
+        const uint64_t bytes = d.n * d.planes * (t.dtype == PBDR_F32 ? 4 : 2);
         r[nr++] = range(t.data, bytes, clip && d.out == t.data);
         if (clip && d.out != t.data) r[nr++] = range(d.out, bytes, true);
         if (t.visible) r[nr++] = range(t.visible, d.n, false);
@@ -276,7 +276,7 @@ static bool to_dev(int32_t count, const pbdr_grad_tensor* list, bool clip, const
 static int grad_workspace_ok(const void* workspace, size_t bytes)
 {
     if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return PBDR_ERR_INVALID_ARG;
-    return bytes < kGradWorkspace ? PBDR_ERR_WORKSPACE_TOO_SMALL : PBDR_OK;
+    return bytes < sizeof(GradWorkspace) ? PBDR_ERR_WORKSPACE_TOO_SMALL : PBDR_OK;
 }
 
 }  // namespace pbdr
@@ -826,7 +826,7 @@ int pbdr_preprocess_bwd_batch_adam(const pbdr_scene* scene, int32_t num_views, c
 int pbdr_grad_workspace_bytes(int32_t num_tensors, size_t* out_bytes)
 {
     if (num_tensors < 0 || num_tensors > PBDR_MAX_GRAD_TENSORS || !out_bytes) return PBDR_ERR_INVALID_ARG;
-    *out_bytes = align256(kGradWorkspace);
+    *out_bytes = align256(sizeof(GradWorkspace));
     return PBDR_OK;
 }
 
@@ -838,9 +838,7 @@ static int grad_impl(int32_t num_tensors, const pbdr_grad_tensor* tensors, float
     if (st != PBDR_OK) return st;
     GradTensorDev list[kGradMaxTensors];
     if (!to_dev(num_tensors, tensors, clip, result, workspace, list)) return PBDR_ERR_INVALID_ARG;
-    hipError_t e = launch_grad_norm(num_tensors, list, max_norm, result, (char*)workspace, (hipStream_t)hip_stream);
-    if (e == hipSuccess && clip) e = launch_grad_scale(num_tensors, list, result, (hipStream_t)hip_stream);
-    return hip_result(e);
+    return hip_result(launch_grad(num_tensors, list, max_norm, result, (GradWorkspace*)workspace, clip, (hipStream_t)hip_stream));
 }
 
 int pbdr_grad_norm(int32_t num_tensors, const pbdr_grad_tensor* tensors, float max_norm, float* result, void* workspace,
@@ -869,10 +867,9 @@ int pbdr_adam_selective_list(int32_t num_tensors, const pbdr_adam_tensor* tensor
     for (int i = 0; i < num_tensors; ++i) {
         const pbdr_adam_tensor& t = tensors[i];
         if (!check_extent(t.n, t.planes) || !(t.lr >= 0.f)) return PBDR_ERR_INVALID_ARG;
-        const AdamDev a = make_adam(t.lr, cfg->beta1, cfg->beta2, cfg->eps, cfg->step, cfg->zero_grad);
-        list[i] = AdamTensorDev{t.param, t.grad, t.exp_avg, t.exp_avg_sq, t.visible, (uint64_t)t.n, (uint64_t)t.n * (uint64_t)t.planes,
-                                (uint32_t)t.planes, 0u, a.step_size};
-        const uint64_t bytes = list[i].count * sizeof(float);
+        const AdamDev a = make_adam(t.lr, cfg->beta1, cfg->beta2, cfg->eps, cfg->step, cfg->zero_grad);      // of which the step size is the tensor's own
+        list[i] = AdamTensorDev{t.param, t.grad, t.exp_avg, t.exp_avg_sq, t.visible, (uint64_t)t.n, (uint32_t)t.planes, 0u, a.step_size};
+        const uint64_t bytes = list[i].n * list[i].planes * sizeof(float);
         if (bytes == 0) continue;
         if (!aligned16(t.param) || !aligned16(t.grad) || !aligned16(t.exp_avg) || !aligned16(t.exp_avg_sq) || (t.visible && !aligned16(t.visible)))
             return PBDR_ERR_INVALID_ARG;

@@ -7,28 +7,31 @@ namespace pbdr {
 enum { kGradF32 = 0, kGradF16 = 1, kGradBF16 = 2 };
 
 constexpr int kGradBlock = 256;
-constexpr int kDenseVecs = 4;
-constexpr int kAdamVecs = 1;
-constexpr uint32_t kMaskPlanes = 8;
-// Planes of a masked unit: Adam reads four vectors a plane, all of a unit before the first is used. At 8M points, a quarter of
-// them used, 3 planes take 914 us with the norm, 4 take 919, 6 take 943, 8 in pairs 926; attributes have 1, 2, 3, 4 or 3K planes.
+constexpr int kDenseVecs = 2;                     // vectors of a lane in a unit of a tensor without mask (2, 4, 8: the same within 2 %)
+// Planes of a masked unit, all of which are read before the first is used. Sums and scaling: 4 (8M points, a quarter used: norm
+// 100 us, clipped into buffers of their own 401; 6 planes 114 and 420; 8 planes 98 and 425). Adam reads four vectors a plane: 3
+// (with the norm 753 us; 1: 766, 2: 751, 4: 757, 6: 790; 1M points: 212, 211, 213, 213, 217); attributes have 1, 2, 3, 4 or 3K planes.
+constexpr uint32_t kMaskPlanes = 4;
 constexpr uint32_t kAdamPlanes = 3;
-constexpr uint32_t kGradBlocks = 2048;            // workgroups of a launch that sums or scales (and one more per tensor at most)
-constexpr uint32_t kAdamBlocks = 1u << 20;        // enough for a unit each: 2,048 workgroups that take several took 10 % longer
-constexpr int kGradTableTensors = 64;             // tensors of one launch: the table is a kernel argument
-constexpr int kAdamTableTensors = 32;
+// Workgroups of a launch that sums or scales, eight per compute unit: units that need no reading leave gaps in masked tensors
+// (8M points, a quarter used: norm 99 us; 1,024 workgroups 113, 512 168; 4,096 103). Tensors without mask take half as many
+// for their units, and stream better so (2M surfels clipped: 239 us against 251).
+constexpr uint32_t kGradBlocks = 2048;
+constexpr uint32_t kMostBlocks = 1u << 23;        // of a launch: fewer than 2^32 threads
+constexpr int kGradTableTensors = 88;             // tensors of one launch: the table is a kernel argument, of 4 KB at most
+constexpr int kAdamTableTensors = 48;
 constexpr int kGradMaxTensors = 1024;             // of a call
 
 struct GradTensorDev {
     const void* data;          // [planes][n]
     void* out;
     const uint8_t* visible;    // [n], or null: all
-    uint64_t n, count;         // count = planes * n
-    uint32_t planes, units;
-    int32_t dtype;
+    uint64_t n;
+    uint32_t planes : 24, dtype : 8;
+    uint32_t units;
 };
 struct GradTable {
-    int count;
+    uint32_t count;
     uint32_t first[kGradTableTensors + 1];        // first workgroup of each tensor, and their number
     GradTensorDev t[kGradTableTensors];
 };
@@ -36,23 +39,33 @@ struct GradTable {
 struct AdamTensorDev {
     float *param, *grad, *m, *v;
     const uint8_t* visible;
-    uint64_t n, count;
+    uint64_t n;
     uint32_t planes, units;
     float step_size;
 };
 struct AdamTable {
-    int count;
+    uint32_t count;
     uint32_t first[kAdamTableTensors + 1];
     AdamDev adam;              // of every tensor but for step_size
     AdamTensorDev t[kAdamTableTensors];
 };
 
-// workspace: the running total, then a slot per workgroup
-constexpr size_t kGradSlotsAt = 256;
-constexpr size_t kGradWorkspace = kGradSlotsAt + (kGradBlocks + kGradTableTensors) * sizeof(double);
+// a slot per workgroup that sums: a table's workgroups are kGradBlocks, one more per tensor where its units do not come out even,
+// and up to seven before each tensor and at the end for the dies' sake
+constexpr uint32_t kGradSlots = kGradBlocks + 8 * (kGradTableTensors + 1);
+// Workgroups up to which one launch sums and finishes: 32 to 128 workgroups 8.3 us a call, 11 with a launch of its own for the
+// end; 250 workgroups 10.5 and 10.3; 500 15.3 and 10.5.
+constexpr uint32_t kAloneSlots = 128;
+// Workgroups up to which every workgroup that scales adds the slots up itself: 128 to 500 workgroups 11.9 us a call, 13.2 to 15.7
+// with a launch between; 1,000 workgroups 12.1 and 15.7; 2,000 16.3 and 15.9.
+constexpr uint32_t kInlineSlots = 1024;
+struct GradWorkspace {
+    uint32_t done;             // workgroups of the running launch that have stored their sum; zero between launches
+    double total;              // of the tables before the running one
+    double slot[kGradSlots];
+};
 
-hipError_t launch_grad_norm(int count, const GradTensorDev* list, float max_norm, float* result, char* ws, hipStream_t s);
-hipError_t launch_grad_scale(int count, const GradTensorDev* list, const float* result, hipStream_t s);
+hipError_t launch_grad(int count, const GradTensorDev* list, float max_norm, float* result, GradWorkspace* ws, bool clip, hipStream_t s);
 hipError_t launch_adam_list(int count, const AdamTensorDev* list, const AdamDev& adam, const float* result, hipStream_t s);
 
 }  // namespace pbdr

@@ -29,19 +29,23 @@ template <class T> struct GradVec {
 };
 
 // the bytes of the mask for kN consecutive points, zero beyond the last point
+template <int kN> struct MaskOf;
+template <> struct MaskOf<4> { using T = uint32_t; };
+template <> struct MaskOf<8> { using T = uint64_t; };
 template <int kN>
-__device__ __forceinline__ uint64_t mask_bytes(const uint8_t* __restrict__ visible, uint64_t at, uint64_t n)
+__device__ __forceinline__ typename MaskOf<kN>::T mask_bytes(const uint8_t* __restrict__ visible, uint64_t at, uint64_t n)
 {
-    if (at + kN <= n) return kN == 4 ? *reinterpret_cast<const uint32_t*>(visible + at) : *reinterpret_cast<const uint64_t*>(visible + at);
-    uint64_t m = 0;
+    using M = typename MaskOf<kN>::T;
+    if (at + kN <= n) return *reinterpret_cast<const M*>(visible + at);
+    M m = 0;
     for (int k = 0; k < kN; ++k)
-        if (at + k < n) m |= (uint64_t)visible[at + k] << (8 * k);
+        if (at + k < n) m |= (M)visible[at + k] << (8 * k);
     return m;
 }
 template <int kN>
-__device__ __forceinline__ bool used(uint64_t mask, int k)
+__device__ __forceinline__ bool used(typename MaskOf<kN>::T mask, int k)
 {
-    return ((kN == 4 ? (uint32_t)mask >> (8 * k) : (uint32_t)(mask >> (8 * k))) & 0xffu) != 0u;
+    return ((uint32_t)(mask >> (8 * k)) & 0xffu) != 0u;
 }
 
 // a unit of a masked tensor: this lane's points and the planes
@@ -52,9 +56,16 @@ struct MaskedUnit {
 template <int kN, uint32_t kPlanes>
 __device__ __forceinline__ MaskedUnit masked_unit(uint32_t u, uint32_t planes)
 {
-    const uint32_t groups = (planes + kPlanes - 1) / kPlanes;
-    const uint32_t seg = u / groups, p0 = (u - seg * groups) * kPlanes;
+    const uint32_t groups = (planes + kPlanes - 1) / kPlanes, eight = u / (8 * groups), in8 = u - eight * 8 * groups;
+    const uint32_t seg = eight * 8 + (in8 & 7), p0 = (in8 >> 3) * kPlanes;
     return MaskedUnit{((uint64_t)seg * kGradBlock + threadIdx.x) * kN, p0, min(p0 + kPlanes, planes)};
+}
+
+template <int kN>
+__device__ __forceinline__ typename MaskOf<kN>::T unit_mask(const GradTensorDev& t, uint32_t u)
+{
+    if (u >= t.units) return 0;
+    return mask_bytes<kN>(t.visible, masked_unit<kN, kMaskPlanes>(u, t.planes).at, t.n);
 }
 
 template <class T>
@@ -78,119 +89,178 @@ __device__ double sum_squares(const GradTensorDev& t, uint32_t first, uint32_t s
     using Vec = typename GradVec<T>::V;
     constexpr int kN = GradVec<T>::kN;
     const T* __restrict__ data = static_cast<const T*>(t.data);
+    const uint64_t count = t.n * t.planes;
     double acc[4] = {0., 0., 0., 0.};
     if (t.visible == nullptr) {
         constexpr uint32_t kUnit = kGradBlock * kN * kDenseVecs;
         for (uint32_t u = first; u < t.units; u += step) {
             const uint64_t base = (uint64_t)u * kUnit + threadIdx.x * kN;
+            if ((uint64_t)(u + 1) * kUnit <= count) {
+                Vec v[kDenseVecs];
 #pragma unroll
-            for (int j = 0; j < kDenseVecs; ++j) {
-                const uint64_t at = base + (uint64_t)j * kGradBlock * kN;
-                if (at + kN <= t.count) {
-                    const Vec v = *reinterpret_cast<const Vec*>(data + at);
+                for (int j = 0; j < kDenseVecs; ++j) v[j] = *reinterpret_cast<const Vec*>(data + base + j * kGradBlock * kN);
 #pragma unroll
-                    for (int k = 0; k < kN; ++k) add_square(acc[k & 3], v[k]);
-                } else {
-                    for (uint64_t i = at; i < t.count; ++i) add_square(acc[0], data[i]);
-                }
+                for (int j = 0; j < kDenseVecs; ++j)
+#pragma unroll
+                    for (int k = 0; k < kN; ++k) add_square(acc[k & 3], (T)v[j][k]);
+            } else {
+                for (int j = 0; j < kDenseVecs; ++j)
+                    for (uint64_t i = base + j * kGradBlock * kN, end = min(i + kN, count); i < end; ++i) add_square(acc[0], data[i]);
             }
         }
     } else {
-        if (first >= t.units) return 0.;
-        MaskedUnit w = masked_unit<kN, kMaskPlanes>(first, t.planes);
-        uint64_t mask = mask_bytes<kN>(t.visible, w.at, t.n);
-        for (uint32_t u = first;;) {
-            // the next unit's mask is on its way while this unit's values come
-            const bool more = u + step < t.units;
-            MaskedUnit w1 = w;
-            uint64_t mask1 = 0;
-            if (more) {
-                w1 = masked_unit<kN, kMaskPlanes>(u + step, t.planes);
-                mask1 = mask_bytes<kN>(t.visible, w1.at, t.n);
+        typename MaskOf<kN>::T next = unit_mask<kN>(t, first);
+        for (uint32_t u = first; u < t.units; u += step) {
+            const typename MaskOf<kN>::T mask = next;
+            next = unit_mask<kN>(t, u + step);      // on its way while this unit's values are
+            if (mask == 0) continue;
+            const MaskedUnit w = masked_unit<kN, kMaskPlanes>(u, t.planes);
+            const T* row = data + (uint64_t)w.p0 * t.n + w.at;
+            if (w.at + kN <= t.n) {
+                Vec v[kMaskPlanes];
+#pragma unroll
+                for (uint32_t i = 0; i < kMaskPlanes; ++i)
+                    if (w.p0 + i < w.p1) v[i] = *reinterpret_cast<const Vec*>(row + (uint64_t)i * t.n);
+#pragma unroll
+                for (uint32_t i = 0; i < kMaskPlanes; ++i)
+                    if (w.p0 + i < w.p1) {
+#pragma unroll
+                        for (int k = 0; k < kN; ++k) add_square(acc[k & 3], used<kN>(mask, k) ? (T)v[i][k] : (T)0.f);
+                    }
+            } else {
+                for (uint32_t p = w.p0; p < w.p1; ++p, row += t.n)
+                    for (int k = 0; k < kN; ++k)
+                        if (used<kN>(mask, k)) add_square(acc[0], row[k]);
             }
-            if (mask != 0) {
-                const T* row = data + (uint64_t)w.p0 * t.n + w.at;
-                if (w.at + kN <= t.n) {
-                    Vec v[kMaskPlanes];
-#pragma unroll
-                    for (uint32_t j = 0; j < kMaskPlanes; ++j)
-                        if (w.p0 + j < w.p1) v[j] = *reinterpret_cast<const Vec*>(row + (uint64_t)j * t.n);
-#pragma unroll
-                    for (uint32_t j = 0; j < kMaskPlanes; ++j)
-                        if (w.p0 + j < w.p1) {
-#pragma unroll
-                            for (int k = 0; k < kN; ++k) add_square(acc[k & 3], used<kN>(mask, k) ? (T)v[j][k] : (T)0.f);
-                        }
-                } else {
-                    for (uint32_t p = w.p0; p < w.p1; ++p, row += t.n)
-                        for (int k = 0; k < kN; ++k)
-                            if (used<kN>(mask, k)) add_square(acc[0], row[k]);
-                }
-            }
-            if (!more) break;
-            u += step;
-            w = w1;
-            mask = mask1;
         }
     }
     return (acc[0] + acc[1]) + (acc[2] + acc[3]);
 }
 
 // the tensor whose workgroups include `block`
-__device__ __forceinline__ int find_tensor(const GradTable& tab, uint32_t block)
+template <class Table>
+__device__ __forceinline__ uint32_t find_tensor(const Table& tab, uint32_t block)
 {
-    int lo = 0, hi = tab.count - 1;
+    uint32_t lo = 0, hi = tab.count - 1;
     while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
+        const uint32_t mid = (lo + hi + 1) >> 1;
         if (tab.first[mid] <= block) lo = mid;
         else hi = mid - 1;
     }
     return lo;
 }
 
-__global__ __launch_bounds__(kGradBlock) void k_grad_squares(GradTable tab, double* __restrict__ slots)
+// what the end of a sum needs
+struct GradEnd {
+    GradWorkspace* ws;
+    float* result;
+    float* norms;              // of the table's tensors
+    float max_norm;
+    int first_table, last_table;
+};
+
+// One workgroup of kThreads: adds the slots of each tensor of the table, and the tensors to the total of the tables before it;
+// returns the factor. All slots are on their way before the first is waited for (one by one they took 8 us instead of 5).
+// The order of the additions depends on the table alone. kAgent: the slots were stored by the running launch.
+template <int kThreads, int kSlots, bool kAgent>
+__device__ __forceinline__ float finish(const GradTable& tab, const GradEnd& end, bool write)
+{
+    __shared__ double sSlot[kSlots];
+    __shared__ double sTensor[kGradTableTensors];
+    __shared__ float sScale;
+    constexpr int kEach = (kSlots + kThreads - 1) / kThreads;
+    const uint32_t count = tab.count, blocks = tab.first[count], lane = threadIdx.x & 63;
+    double mine[kEach];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const uint32_t i = j * kThreads + threadIdx.x;
+        mine[j] = i >= blocks ? 0. : kAgent ? __hip_atomic_load(&end.ws->slot[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : end.ws->slot[i];
+    }
+#pragma unroll
+    for (int j = 0; j < kEach; ++j)
+        if (j * kThreads + threadIdx.x < kSlots) sSlot[j * kThreads + threadIdx.x] = mine[j];
+    __syncthreads();
+    // tensors of few slots: sixteen lanes each
+    for (uint32_t t = threadIdx.x >> 4; t < count; t += kThreads / 16) {
+        const uint32_t from = tab.first[t], to = tab.first[t + 1];
+        if (to - from > 64) continue;
+        double s = 0.;
+        for (uint32_t i = from + (lane & 15); i < to; i += 16) s += sSlot[i];
+#pragma unroll
+        for (int d = 8; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
+        if ((lane & 15) == 0) sTensor[t] = s;
+    }
+    for (uint32_t t = threadIdx.x >> 6; t < count; t += kThreads / 64) {
+        const uint32_t from = tab.first[t], to = tab.first[t + 1];
+        if (to - from <= 64) continue;
+        double s = 0.;
+        for (uint32_t i = from + lane; i < to; i += 64) s += sSlot[i];
+        s = wave_sum(s);
+        if (lane == 0) sTensor[t] = s;
+    }
+    __syncthreads();
+    if (write && threadIdx.x < count) end.norms[threadIdx.x] = (float)sqrt(sTensor[threadIdx.x]);
+    if (threadIdx.x < 64) {
+        double s = 0.;
+        for (uint32_t t = lane; t < count; t += 64) s += sTensor[t];
+        s = wave_sum(s);
+        if (lane == 0) {
+            if (!end.first_table) s += end.ws->total;
+            const double norm = sqrt(s);
+            const float scale = !(norm <= 1.7976931348623157e308) ? 0.f : norm > (double)end.max_norm ? (float)((double)end.max_norm / norm) : 1.f;
+            sScale = scale;
+            if (write && end.last_table) {
+                end.result[0] = (float)norm;
+                end.result[1] = scale;
+            } else if (write) {
+                end.ws->total = s;
+            }
+        }
+    }
+    __syncthreads();
+    return sScale;
+}
+
+__global__ __launch_bounds__(1024) void k_grad_finish(GradTable tab, GradEnd end)
+{
+    finish<1024, kGradSlots, false>(tab, end, true);
+}
+
+// Every workgroup sums its part into a slot. kAlone: the last one to be done finishes in the same launch: slots go past the
+// caches of the eight dies (agent scope), and the counter is left at zero for the next launch.
+template <bool kAlone>
+__global__ __launch_bounds__(kGradBlock, 8) void k_grad_squares(GradTable tab, GradEnd end)
 {
     __shared__ double sWave[kGradBlock / 64];
-    const int ti = find_tensor(tab, blockIdx.x);
-    const GradTensorDev& t = tab.t[ti];
-    const uint32_t first = blockIdx.x - tab.first[ti], step = tab.first[ti + 1] - tab.first[ti];
-    double s;
-    if (t.dtype == kGradF32) s = sum_squares<kGradF32>(t, first, step);
-    else if (t.dtype == kGradF16) s = sum_squares<kGradF16>(t, first, step);
-    else s = sum_squares<kGradBF16>(t, first, step);
-    s = wave_sum(s);
-    if ((threadIdx.x & 63) == 0) sWave[threadIdx.x >> 6] = s;
+    __shared__ bool sLast;
+    if (!kAlone || tab.first[tab.count]) {      // else one workgroup has come to write the norm of nothing
+        const uint32_t ti = find_tensor(tab, blockIdx.x);
+        const GradTensorDev& t = tab.t[ti];
+        const uint32_t first = blockIdx.x - tab.first[ti], step = tab.first[ti + 1] - tab.first[ti];
+        double s;
+        if (t.dtype == kGradF32) s = sum_squares<kGradF32>(t, first, step);
+        else if (t.dtype == kGradF16) s = sum_squares<kGradF16>(t, first, step);
+        else s = sum_squares<kGradBF16>(t, first, step);
+        s = wave_sum(s);
+        if ((threadIdx.x & 63) == 0) sWave[threadIdx.x >> 6] = s;
+    }
     __syncthreads();
     if (threadIdx.x == 0) {
         double r = sWave[0];
         for (int w = 1; w < kGradBlock / 64; ++w) r += sWave[w];
-        slots[blockIdx.x] = r;
-    }
-}
-
-// One workgroup: adds the slots of each tensor of the table, and the tensors to the total of the tables before it.
-__global__ __launch_bounds__(1024) void k_grad_finish(GradTable tab, const double* __restrict__ slots, double* __restrict__ total, int first_table,
-                                                      int last_table, float max_norm, float* __restrict__ result, float* __restrict__ norms)
-{
-    __shared__ double sTensor[kGradTableTensors];
-    for (int t = threadIdx.x >> 6; t < tab.count; t += 16) {
-        double s = 0.;
-        for (uint32_t i = tab.first[t] + (threadIdx.x & 63); i < tab.first[t + 1]; i += 64) s += slots[i];
-        s = wave_sum(s);
-        if ((threadIdx.x & 63) == 0) {
-            sTensor[t] = s;
-            norms[t] = (float)sqrt(s);
+        if (kAlone) {
+            __hip_atomic_store(&end.ws->slot[blockIdx.x], r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            sLast = __hip_atomic_fetch_add(&end.ws->done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+        } else {
+            end.ws->slot[blockIdx.x] = r;
         }
     }
+    if (!kAlone) return;
     __syncthreads();
-    if (threadIdx.x != 0) return;
-    double sum = first_table ? 0. : *total;
-    for (int t = 0; t < tab.count; ++t) sum += sTensor[t];
-    *total = sum;
-    if (!last_table) return;
-    const double norm = sqrt(sum);
-    result[0] = (float)norm;
-    result[1] = !(norm <= 1.7976931348623157e308) ? 0.f : norm > (double)max_norm ? (float)((double)max_norm / norm) : 1.f;
+    if (!sLast) return;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    finish<kGradBlock, kAloneSlots, true>(tab, end, true);
+    if (threadIdx.x == 0) __hip_atomic_store(&end.ws->done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // scale * g in fp32, rounded once more to the tensor's type; a factor of zero makes zeros of everything, NaN and infinities included
@@ -198,6 +268,13 @@ template <class T>
 __device__ __forceinline__ T scaled(T g, float scale)
 {
     return scale == 0.f ? (T)0.f : (T)((float)g * scale);
+}
+
+// what is written is not read again here: it leaves the last-level cache to the gradient
+template <class Vec, class T>
+__device__ __forceinline__ void store_vec(Vec v, T* to)
+{
+    __builtin_nontemporal_store(v, reinterpret_cast<Vec*>(to));
 }
 
 template <int kDtype>
@@ -208,48 +285,52 @@ __device__ void write_scaled(const GradTensorDev& t, float scale, uint32_t first
     constexpr int kN = GradVec<T>::kN;
     const T* data = static_cast<const T*>(t.data);      // may be the output
     T* out = static_cast<T*>(t.out);
+    const uint64_t count = t.n * t.planes;
     if (t.visible == nullptr) {
         constexpr uint32_t kUnit = kGradBlock * kN * kDenseVecs;
         for (uint32_t u = first; u < t.units; u += step) {
             const uint64_t base = (uint64_t)u * kUnit + threadIdx.x * kN;
+            if ((uint64_t)(u + 1) * kUnit <= count) {
+                Vec v[kDenseVecs];
 #pragma unroll
-            for (int j = 0; j < kDenseVecs; ++j) {
-                const uint64_t at = base + (uint64_t)j * kGradBlock * kN;
-                if (at + kN <= t.count) {
-                    Vec v = *reinterpret_cast<const Vec*>(data + at);
+                for (int j = 0; j < kDenseVecs; ++j) v[j] = *reinterpret_cast<const Vec*>(data + base + j * kGradBlock * kN);
 #pragma unroll
-                    for (int k = 0; k < kN; ++k) v[k] = scaled((T)v[k], scale);
-                    *reinterpret_cast<Vec*>(out + at) = v;
-                } else {
-                    for (uint64_t i = at; i < t.count; ++i) out[i] = scaled(data[i], scale);
+                for (int j = 0; j < kDenseVecs; ++j) {
+#pragma unroll
+                    for (int k = 0; k < kN; ++k) v[j][k] = scaled((T)v[j][k], scale);
+                    store_vec(v[j], out + base + j * kGradBlock * kN);
                 }
+            } else {
+                for (int j = 0; j < kDenseVecs; ++j)
+                    for (uint64_t i = base + j * kGradBlock * kN, end = min(i + kN, count); i < end; ++i) out[i] = scaled(data[i], scale);
             }
         }
     } else {
         for (uint32_t u = first; u < t.units; u += step) {
             const MaskedUnit w = masked_unit<kN, kMaskPlanes>(u, t.planes);
-            const uint64_t mask = mask_bytes<kN>(t.visible, w.at, t.n);
+            const typename MaskOf<kN>::T mask = mask_bytes<kN>(t.visible, w.at, t.n);
             if (mask == 0) continue;
-            bool all = true;
-#pragma unroll
-            for (int k = 0; k < kN; ++k) all = all && used<kN>(mask, k);
             const uint64_t o = (uint64_t)w.p0 * t.n + w.at;
             if (w.at + kN <= t.n) {
-                Vec v[kMaskPlanes];
+                bool all = true;
+#pragma unroll
+                for (int k = 0; k < kN; ++k) all = all && used<kN>(mask, k);
+                Vec v[kMaskPlanes], old[kMaskPlanes];
 #pragma unroll
                 for (uint32_t j = 0; j < kMaskPlanes; ++j)
-                    if (w.p0 + j < w.p1) v[j] = *reinterpret_cast<const Vec*>(data + o + (uint64_t)j * t.n);
+                    if (w.p0 + j < w.p1) old[j] = v[j] = *reinterpret_cast<const Vec*>(data + o + (uint64_t)j * t.n);
+                // an unused entry among used ones is read and written back: stores that leave holes in a line cost the memory more
+                if (!all && out != data) {
+#pragma unroll
+                    for (uint32_t j = 0; j < kMaskPlanes; ++j)
+                        if (w.p0 + j < w.p1) old[j] = *reinterpret_cast<const Vec*>(out + o + (uint64_t)j * t.n);
+                }
 #pragma unroll
                 for (uint32_t j = 0; j < kMaskPlanes; ++j)
                     if (w.p0 + j < w.p1) {
-                        T* to = out + o + (uint64_t)j * t.n;
 #pragma unroll
-                        for (int k = 0; k < kN; ++k) v[j][k] = scaled((T)v[j][k], scale);
-                        if (all) *reinterpret_cast<Vec*>(to) = v[j];
-                        else
-#pragma unroll
-                            for (int k = 0; k < kN; ++k)
-                                if (used<kN>(mask, k)) to[k] = v[j][k];
+                        for (int k = 0; k < kN; ++k) v[j][k] = used<kN>(mask, k) ? scaled((T)v[j][k], scale) : (T)old[j][k];
+                        store_vec(v[j], out + o + (uint64_t)j * t.n);
                     }
             } else {
                 for (uint32_t p = w.p0; p < w.p1; ++p)
@@ -262,13 +343,16 @@ __device__ void write_scaled(const GradTensorDev& t, float scale, uint32_t first
     }
 }
 
-__global__ __launch_bounds__(kGradBlock) void k_grad_scale(GradTable tab, const float* __restrict__ result)
+// kFinish: every workgroup adds the slots up for itself, one writes the result: for small lists, whose sums then need no ending
+template <bool kFinish>
+__global__ __launch_bounds__(kGradBlock) void k_grad_scale(GradTable tab, GradEnd end)
 {
-    const int ti = find_tensor(tab, blockIdx.x);
+    const uint32_t block = gridDim.x - 1 - blockIdx.x;      // backwards: the end of the gradient was read last
+    const uint32_t ti = find_tensor(tab, block);
     const GradTensorDev& t = tab.t[ti];
-    const float scale = result[1];
+    const float scale = kFinish ? finish<kGradBlock, kInlineSlots, false>(tab, end, blockIdx.x == 0) : end.result[1];
     if (scale == 1.f && t.out == t.data) return;      // nothing would change
-    const uint32_t first = blockIdx.x - tab.first[ti], step = tab.first[ti + 1] - tab.first[ti];
+    const uint32_t first = block - tab.first[ti], step = tab.first[ti + 1] - tab.first[ti];
     if (t.dtype == kGradF32) write_scaled<kGradF32>(t, scale, first, step);
     else if (t.dtype == kGradF16) write_scaled<kGradF16>(t, scale, first, step);
     else write_scaled<kGradBF16>(t, scale, first, step);
@@ -290,8 +374,9 @@ struct AdamVec {
 __device__ __forceinline__ AdamVec adam_load(const AdamTensorDev& t, uint64_t at)
 {
     using Vec = GradVec<float>::V;
-    return AdamVec{*reinterpret_cast<const Vec*>(t.param + at), *reinterpret_cast<const Vec*>(t.grad + at), *reinterpret_cast<const Vec*>(t.m + at),
-                   *reinterpret_cast<const Vec*>(t.v + at)};
+    // parameters and moments pass by the last-level cache, which holds part of the gradient that the norm has just read
+    return AdamVec{__builtin_nontemporal_load(reinterpret_cast<const Vec*>(t.param + at)), *reinterpret_cast<const Vec*>(t.grad + at),
+                   __builtin_nontemporal_load(reinterpret_cast<const Vec*>(t.m + at)), __builtin_nontemporal_load(reinterpret_cast<const Vec*>(t.v + at))};
 }
 __device__ __forceinline__ void adam_store(const AdamDev& c, float scale, uint32_t mask, const AdamTensorDev& t, uint64_t at, AdamVec x)
 {
@@ -304,41 +389,33 @@ __device__ __forceinline__ void adam_store(const AdamDev& c, float scale, uint32
             x.p[k] = a; x.m[k] = b; x.v[k] = d; x.g[k] = 0.f;
         }
     }
-    *reinterpret_cast<Vec*>(t.param + at) = x.p;
-    *reinterpret_cast<Vec*>(t.m + at) = x.m;
-    *reinterpret_cast<Vec*>(t.v + at) = x.v;
+    __builtin_nontemporal_store(x.p, reinterpret_cast<Vec*>(t.param + at));
+    __builtin_nontemporal_store(x.m, reinterpret_cast<Vec*>(t.m + at));
+    __builtin_nontemporal_store(x.v, reinterpret_cast<Vec*>(t.v + at));
     if (c.zero_grad) *reinterpret_cast<Vec*>(t.grad + at) = x.g;
 }
 
 __global__ __launch_bounds__(kGradBlock) void k_adam_list(AdamTable tab, const float* __restrict__ result)
 {
-    int lo = 0, hi = tab.count - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (tab.first[mid] <= blockIdx.x) lo = mid;
-        else hi = mid - 1;
-    }
-    const AdamTensorDev& t = tab.t[lo];
+    const uint32_t block = gridDim.x - 1 - blockIdx.x;      // backwards: the norm has read the end of the gradient last
+    const uint32_t ti = find_tensor(tab, block);
+    const AdamTensorDev& t = tab.t[ti];
     const float scale = result ? result[1] : 1.f;
     AdamDev c = tab.adam;
     c.step_size = t.step_size;
-    const uint32_t first = blockIdx.x - tab.first[lo], step = tab.first[lo + 1] - tab.first[lo];
+    const uint32_t first = block - tab.first[ti], step = tab.first[ti + 1] - tab.first[ti];
     if (t.visible == nullptr) {
-        constexpr uint32_t kUnit = kGradBlock * 4 * kAdamVecs;
+        const uint64_t count = t.n * t.planes;
         for (uint32_t u = first; u < t.units; u += step) {
-            const uint64_t base = (uint64_t)u * kUnit + threadIdx.x * 4;
-#pragma unroll
-            for (int j = 0; j < kAdamVecs; ++j) {
-                const uint64_t at = base + (uint64_t)j * kGradBlock * 4;
-                if (at + 4 <= t.count) adam_store(c, scale, ~0u, t, at, adam_load(t, at));
-                else
-                    for (uint64_t i = at; i < t.count; ++i) adam_clipped(c, scale, t.param + i, t.grad + i, t.m + i, t.v + i);
-            }
+            const uint64_t at = ((uint64_t)u * kGradBlock + threadIdx.x) * 4;
+            if (at + 4 <= count) adam_store(c, scale, ~0u, t, at, adam_load(t, at));
+            else
+                for (uint64_t i = at; i < count; ++i) adam_clipped(c, scale, t.param + i, t.grad + i, t.m + i, t.v + i);
         }
     } else {
         for (uint32_t u = first; u < t.units; u += step) {
             const MaskedUnit w = masked_unit<4, kAdamPlanes>(u, t.planes);
-            const uint32_t mask = (uint32_t)mask_bytes<4>(t.visible, w.at, t.n);
+            const uint32_t mask = mask_bytes<4>(t.visible, w.at, t.n);
             if (mask == 0) continue;
             uint64_t at = (uint64_t)w.p0 * t.n + w.at;
             if (w.at + 4 <= t.n) {
@@ -358,66 +435,83 @@ __global__ __launch_bounds__(kGradBlock) void k_adam_list(AdamTable tab, const f
     }
 }
 
-// Units of a tensor, and how many workgroups share the units of a table: one unit each up to kGradBlocks of them, then equal runs.
+static uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+
+// units of a tensor whose vectors have `vec` values
 template <class T>
-static void cut_units(T& t, int value_bytes, int dense_vecs, uint32_t planes)
+static void cut_units(T& t, uint64_t vec, uint64_t dense_vecs, uint32_t planes)
 {
-    const uint64_t vec = 16 / value_bytes;
-    if (t.count == 0) t.units = 0;
-    else if (t.visible == nullptr) t.units = (uint32_t)((t.count + kGradBlock * vec * dense_vecs - 1) / (kGradBlock * vec * dense_vecs));
-    else t.units = (uint32_t)((t.n + kGradBlock * vec - 1) / (kGradBlock * vec)) * ((t.planes + planes - 1) / planes);
+    if (t.n == 0 || t.planes == 0) t.units = 0;
+    else if (t.visible == nullptr) t.units = (uint32_t)ceil_div(t.n * t.planes, kGradBlock * vec * dense_vecs);
+    else t.units = (uint32_t)(ceil_div(t.n, kGradBlock * vec * 8) * 8 * ceil_div(t.planes, planes));
 }
 
+// The workgroups of a table: one per unit, or, with more than `most` units, equal runs of them.
 template <class Table>
-static uint32_t cut_blocks(Table& tab, uint32_t most)
+static uint32_t cut_blocks(Table& tab, uint64_t units, uint32_t most)
 {
-    uint64_t units = 0;
-    for (int i = 0; i < tab.count; ++i) units += tab.t[i].units;
-    const uint64_t each = units > most ? (units + most - 1) / most : 1;
+    const uint64_t each = units > most ? ceil_div(units, most) : 1;
     uint32_t at = 0;
-    for (int i = 0; i < tab.count; ++i) {
+    for (uint32_t i = 0; i < tab.count; ++i) {
+        if (tab.t[i].visible && tab.t[i].units >= 64) at = (at + 7) & ~7u;      // for the dies, see masked_unit()
         tab.first[i] = at;
-        at += (uint32_t)((tab.t[i].units + each - 1) / each);
+        at += (uint32_t)ceil_div(tab.t[i].units, tab.t[i].visible || each == 1 ? each : 2 * each);
     }
+    if (units >= 64) at = (at + 7) & ~7u;
     tab.first[tab.count] = at;
     return at;
 }
 
-// A table of up to kGradTableTensors of the list; tensors without entries keep their place and get no workgroup.
-static uint32_t fill_table(GradTable& tab, const GradTensorDev* list, int count)
+// Up to kGradTableTensors of a list; tensors without entries keep their place and get no unit.
+static uint64_t fill_table(GradTable& tab, const GradTensorDev* list, int count)
 {
-    tab.count = count;
-    for (int i = 0; i < count; ++i) {
+    uint64_t units = 0;
+    tab.count = (uint32_t)(count < kGradTableTensors ? count : kGradTableTensors);
+    for (uint32_t i = 0; i < tab.count; ++i) {
         tab.t[i] = list[i];
-        cut_units(tab.t[i], list[i].dtype == kGradF32 ? 4 : 2, kDenseVecs, kMaskPlanes);
+        cut_units(tab.t[i], list[i].dtype == kGradF32 ? 4 : 8, kDenseVecs, kMaskPlanes);
+        units += tab.t[i].units;
     }
-    return cut_blocks(tab, kGradBlocks);
+    return units;
 }
 
-hipError_t launch_grad_norm(int count, const GradTensorDev* list, float max_norm, float* result, char* ws, hipStream_t s)
-{
-    double* total = reinterpret_cast<double*>(ws);
-    double* slots = reinterpret_cast<double*>(ws + kGradSlotsAt);
-    int at = 0;
-    ProfScope prof(kKGradNorm, s);
-    do {
-        GradTable tab;
-        const int part = count - at < kGradTableTensors ? count - at : kGradTableTensors;
-        const uint32_t blocks = fill_table(tab, list + at, part);
-        if (blocks) hipLaunchKernelGGL(k_grad_squares, dim3(blocks), dim3(kGradBlock), 0, s, tab, slots);
-        hipLaunchKernelGGL(k_grad_finish, dim3(1), dim3(1024), 0, s, tab, slots, total, at == 0, at + part == count, max_norm, result, result + 2 + at);
-        at += part;
-    } while (at < count);
-    return hipGetLastError();
-}
+template <class Args>
+constexpr bool fits_kernel_arguments() { return sizeof(Args) + sizeof(GradEnd) <= 4096; }
+static_assert(fits_kernel_arguments<GradTable>() && fits_kernel_arguments<AdamTable>(), "");
 
-hipError_t launch_grad_scale(int count, const GradTensorDev* list, const float* result, hipStream_t s)
+hipError_t launch_grad(int count, const GradTensorDev* list, float max_norm, float* result, GradWorkspace* ws, bool clip, hipStream_t s)
 {
-    ProfScope prof(kKGradScale, s);
-    for (int at = 0; at < count; at += kGradTableTensors) {
-        GradTable tab;
-        const uint32_t blocks = fill_table(tab, list + at, count - at < kGradTableTensors ? count - at : kGradTableTensors);
-        if (blocks) hipLaunchKernelGGL(k_grad_scale, dim3(blocks), dim3(kGradBlock), 0, s, tab, result);
+    GradTable tab;
+    bool scaled = !clip;
+    {
+        ProfScope prof(kKGradNorm, s);
+        int at = 0;
+        do {
+            const uint64_t units = fill_table(tab, list + at, count - at);
+            const uint32_t blocks = cut_blocks(tab, units, kGradBlocks);
+            const GradEnd end{ws, result, result + 2 + at, max_norm, at == 0, at + (int)tab.count == count};
+            const dim3 grid(blocks ? blocks : 1), block(kGradBlock);
+            if (blocks && blocks <= kInlineSlots && clip && end.first_table && end.last_table) {
+                hipLaunchKernelGGL(k_grad_squares<false>, grid, block, 0, s, tab, end);
+                hipLaunchKernelGGL(k_grad_scale<true>, grid, block, 0, s, tab, end);
+                scaled = true;
+            } else if (blocks <= kAloneSlots) {
+                hipLaunchKernelGGL(k_grad_squares<true>, grid, block, 0, s, tab, end);
+            } else {
+                hipLaunchKernelGGL(k_grad_squares<false>, grid, block, 0, s, tab, end);
+                hipLaunchKernelGGL(k_grad_finish, dim3(1), dim3(1024), 0, s, tab, end);
+            }
+            at += (int)tab.count;
+        } while (at < count);
+    }
+    if (!scaled) {
+        ProfScope prof(kKGradScale, s);
+        for (int at = 0; at < count; at += (int)tab.count) {
+            const uint64_t units = fill_table(tab, list + at, count - at);
+            const uint32_t blocks = cut_blocks(tab, units, kMostBlocks);
+            const GradEnd end{ws, result, result + 2 + at, max_norm, 0, 0};
+            if (blocks) hipLaunchKernelGGL(k_grad_scale<false>, dim3(blocks), dim3(kGradBlock), 0, s, tab, end);
+        }
     }
     return hipGetLastError();
 }
@@ -425,15 +519,17 @@ hipError_t launch_grad_scale(int count, const GradTensorDev* list, const float* 
 hipError_t launch_adam_list(int count, const AdamTensorDev* list, const AdamDev& adam, const float* result, hipStream_t s)
 {
     ProfScope prof(kKAdamList, s);
-    for (int at = 0; at < count; at += kAdamTableTensors) {
-        AdamTable tab;
-        tab.adam = adam;
-        tab.count = count - at < kAdamTableTensors ? count - at : kAdamTableTensors;
-        for (int i = 0; i < tab.count; ++i) {
+    AdamTable tab;
+    tab.adam = adam;
+    for (int at = 0; at < count; at += (int)tab.count) {
+        uint64_t units = 0;
+        tab.count = (uint32_t)(count - at < kAdamTableTensors ? count - at : kAdamTableTensors);
+        for (uint32_t i = 0; i < tab.count; ++i) {
             tab.t[i] = list[at + i];
-            cut_units(tab.t[i], 4, kAdamVecs, kAdamPlanes);
+            cut_units(tab.t[i], 4, 1, kAdamPlanes);
+            units += tab.t[i].units;
         }
-        const uint32_t blocks = cut_blocks(tab, kAdamBlocks);
+        const uint32_t blocks = cut_blocks(tab, units, kMostBlocks);
         if (blocks) hipLaunchKernelGGL(k_adam_list, dim3(blocks), dim3(kGradBlock), 0, s, tab, result);
     }
     return hipGetLastError();

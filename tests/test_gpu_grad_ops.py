@@ -75,7 +75,6 @@ def check_clipped(out, before, t, mask, factor):
 
 def run_clip(ts, ms, max_norm, in_place=False):
     ws = B.alloc_grad_workspace(len(ts))
-    ws.fill_(255)      # needs no clearing
     result = torch.full((2 + len(ts),), 9.0, device="cuda")
     raw = [t.clone() for t in ts]
     out = None if in_place else [torch.full_like(t, 7.0) for t in ts]
