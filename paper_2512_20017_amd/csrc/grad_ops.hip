@@ -491,7 +491,7 @@ hipError_t launch_grad(int count, const GradTensorDev* list, float max_norm, flo
             const uint32_t blocks = cut_blocks(tab, units, kGradBlocks);
             const GradEnd end{ws, result, result + 2 + at, max_norm, at == 0, at + (int)tab.count == count};
             const dim3 grid(blocks ? blocks : 1), block(kGradBlock);
-            if (blocks && blocks <= kInlineSlots && clip && end.first_table && end.last_table) {
+            if (blocks && blocks <= kInlineSlots && units <= kGradBlocks && clip && end.first_table && end.last_table) {      // a workgroup per unit
                 hipLaunchKernelGGL(k_grad_squares<false>, grid, block, 0, s, tab, end);
                 hipLaunchKernelGGL(k_grad_scale<true>, grid, block, 0, s, tab, end);
                 scaled = true;
