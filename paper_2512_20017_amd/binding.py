@@ -529,14 +529,16 @@ def _call_on(device, stream, entry, *args) -> None:
     if device.type != "cuda":
         raise ValueError(f"pbdr: tensors lie on {device}, not on a GPU")
     if stream is None:
-        stream = torch.cuda.current_stream(device)
+        handle = torch._C._cuda_getCurrentRawStream(device.index)      # what torch.cuda.current_stream(device) wraps up in 2 us
     elif stream.device != device:
         raise ValueError(f"pbdr: a stream of {stream.device} for tensors on {device}")
+    else:
+        handle = stream.cuda_stream
     if device.index == torch.cuda.current_device():
-        _check(entry(*args, stream.cuda_stream))
+        _check(entry(*args, handle))
     else:
         with torch.cuda.device(device):
-            _check(entry(*args, stream.cuda_stream))
+            _check(entry(*args, handle))
 
 
 def _result_address(result, count, device):

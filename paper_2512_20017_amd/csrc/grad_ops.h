@@ -31,7 +31,7 @@ struct GradTensorDev {
     uint32_t units;
 };
 struct GradTable {
-    uint32_t count;
+    uint32_t count, blocks;
     uint32_t first[kGradTableTensors + 1];        // first workgroup of each tensor, and their number
     GradTensorDev t[kGradTableTensors];
 };
@@ -44,7 +44,7 @@ struct AdamTensorDev {
     float step_size;
 };
 struct AdamTable {
-    uint32_t count;
+    uint32_t count, blocks;
     uint32_t first[kAdamTableTensors + 1];
     AdamDev adam;              // of every tensor but for step_size
     AdamTensorDev t[kAdamTableTensors];

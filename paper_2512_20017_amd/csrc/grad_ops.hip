@@ -12,6 +12,7 @@
 // lane. With a mask a unit is one vector of points per lane and up to kMaskPlanes planes: the mask is read once for all of them,
 // and a lane that has no used point reads nothing else. A lane that has one reads whole vectors, all planes of the unit at once.
 #include "grad_ops.h"
+#include "wave_ops.h"
 
 #include <cmath>
 
@@ -28,6 +29,18 @@ template <class T> struct GradVec {
     typedef T V __attribute__((ext_vector_type(kN), aligned(sizeof(T))));
 };
 
+// The end of a row: values at and after `at`, zero beyond its n values. One round trip: what lies beyond reads the last value.
+template <class T>
+__device__ __forceinline__ typename GradVec<T>::V load_end(const T* row, uint64_t at, uint64_t n)
+{
+    typename GradVec<T>::V v;
+#pragma unroll
+    for (int k = 0; k < GradVec<T>::kN; ++k) v[k] = row[min(at + k, n - 1)];
+#pragma unroll
+    for (int k = 0; k < GradVec<T>::kN; ++k) v[k] = at + k < n ? (T)v[k] : (T)0.f;
+    return v;
+}
+
 // the bytes of the mask for kN consecutive points, zero beyond the last point
 template <int kN> struct MaskOf;
 template <> struct MaskOf<4> { using T = uint32_t; };
@@ -37,9 +50,13 @@ __device__ __forceinline__ typename MaskOf<kN>::T mask_bytes(const uint8_t* __re
 {
     using M = typename MaskOf<kN>::T;
     if (at + kN <= n) return *reinterpret_cast<const M*>(visible + at);
+    if (at >= n) return 0;
+    uint8_t byte[kN];
+#pragma unroll
+    for (int k = 0; k < kN; ++k) byte[k] = visible[min(at + k, n - 1)];
     M m = 0;
-    for (int k = 0; k < kN; ++k)
-        if (at + k < n) m |= (M)visible[at + k] << (8 * k);
+#pragma unroll
+    for (int k = 0; k < kN; ++k) m |= at + k < n ? (M)byte[k] << (8 * k) : (M)0;
     return m;
 }
 template <int kN>
@@ -75,13 +92,6 @@ __device__ __forceinline__ void add_square(double& acc, T v)
     acc = fma(d, d, acc);
 }
 
-__device__ __forceinline__ double wave_sum(double v)
-{
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d, 64);
-    return v;
-}
-
 template <int kDtype>
 __device__ double sum_squares(const GradTensorDev& t, uint32_t first, uint32_t step)
 {
@@ -95,18 +105,18 @@ __device__ double sum_squares(const GradTensorDev& t, uint32_t first, uint32_t s
         constexpr uint32_t kUnit = kGradBlock * kN * kDenseVecs;
         for (uint32_t u = first; u < t.units; u += step) {
             const uint64_t base = (uint64_t)u * kUnit + threadIdx.x * kN;
+            Vec v[kDenseVecs];
             if ((uint64_t)(u + 1) * kUnit <= count) {
-                Vec v[kDenseVecs];
 #pragma unroll
                 for (int j = 0; j < kDenseVecs; ++j) v[j] = *reinterpret_cast<const Vec*>(data + base + j * kGradBlock * kN);
-#pragma unroll
-                for (int j = 0; j < kDenseVecs; ++j)
-#pragma unroll
-                    for (int k = 0; k < kN; ++k) add_square(acc[k & 3], (T)v[j][k]);
             } else {
-                for (int j = 0; j < kDenseVecs; ++j)
-                    for (uint64_t i = base + j * kGradBlock * kN, end = min(i + kN, count); i < end; ++i) add_square(acc[0], data[i]);
+#pragma unroll
+                for (int j = 0; j < kDenseVecs; ++j) v[j] = load_end(data, base + j * kGradBlock * kN, count);
             }
+#pragma unroll
+            for (int j = 0; j < kDenseVecs; ++j)
+#pragma unroll
+                for (int k = 0; k < kN; ++k) add_square(acc[k & 3], (T)v[j][k]);
         }
     } else {
         typename MaskOf<kN>::T next = unit_mask<kN>(t, first);
@@ -115,23 +125,23 @@ __device__ double sum_squares(const GradTensorDev& t, uint32_t first, uint32_t s
             next = unit_mask<kN>(t, u + step);      // on its way while this unit's values are
             if (mask == 0) continue;
             const MaskedUnit w = masked_unit<kN, kMaskPlanes>(u, t.planes);
-            const T* row = data + (uint64_t)w.p0 * t.n + w.at;
+            const T* row = data + (uint64_t)w.p0 * t.n;
+            Vec v[kMaskPlanes];
             if (w.at + kN <= t.n) {
-                Vec v[kMaskPlanes];
 #pragma unroll
                 for (uint32_t i = 0; i < kMaskPlanes; ++i)
-                    if (w.p0 + i < w.p1) v[i] = *reinterpret_cast<const Vec*>(row + (uint64_t)i * t.n);
-#pragma unroll
-                for (uint32_t i = 0; i < kMaskPlanes; ++i)
-                    if (w.p0 + i < w.p1) {
-#pragma unroll
-                        for (int k = 0; k < kN; ++k) add_square(acc[k & 3], used<kN>(mask, k) ? (T)v[i][k] : (T)0.f);
-                    }
+                    if (w.p0 + i < w.p1) v[i] = *reinterpret_cast<const Vec*>(row + i * t.n + w.at);
             } else {
-                for (uint32_t p = w.p0; p < w.p1; ++p, row += t.n)
-                    for (int k = 0; k < kN; ++k)
-                        if (used<kN>(mask, k)) add_square(acc[0], row[k]);
+#pragma unroll
+                for (uint32_t i = 0; i < kMaskPlanes; ++i)
+                    if (w.p0 + i < w.p1) v[i] = load_end(row + i * t.n, w.at, t.n);
             }
+#pragma unroll
+            for (uint32_t i = 0; i < kMaskPlanes; ++i)
+                if (w.p0 + i < w.p1) {
+#pragma unroll
+                    for (int k = 0; k < kN; ++k) add_square(acc[k & 3], used<kN>(mask, k) ? (T)v[i][k] : (T)0.f);
+                }
         }
     }
     return (acc[0] + acc[1]) + (acc[2] + acc[3]);
@@ -167,33 +177,36 @@ __device__ __forceinline__ float finish(const GradTable& tab, const GradEnd& end
 {
     __shared__ double sSlot[kSlots];
     __shared__ double sTensor[kGradTableTensors];
+    __shared__ uint32_t sFirst[kGradTableTensors + 1];
     __shared__ float sScale;
+    static_assert(kThreads > kGradTableTensors, "");
     constexpr int kEach = (kSlots + kThreads - 1) / kThreads;
-    const uint32_t count = tab.count, blocks = tab.first[count], lane = threadIdx.x & 63;
+    const uint32_t count = tab.count, blocks = tab.blocks, lane = threadIdx.x & 63;
     double mine[kEach];
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
         const uint32_t i = j * kThreads + threadIdx.x;
         mine[j] = i >= blocks ? 0. : kAgent ? __hip_atomic_load(&end.ws->slot[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : end.ws->slot[i];
     }
+    if (threadIdx.x <= count) sFirst[threadIdx.x] = tab.first[threadIdx.x];
 #pragma unroll
     for (int j = 0; j < kEach; ++j)
         if (j * kThreads + threadIdx.x < kSlots) sSlot[j * kThreads + threadIdx.x] = mine[j];
     __syncthreads();
     // tensors of few slots: sixteen lanes each
     for (uint32_t t = threadIdx.x >> 4; t < count; t += kThreads / 16) {
-        const uint32_t from = tab.first[t], to = tab.first[t + 1];
+        const uint32_t from = sFirst[t], to = sFirst[t + 1];
         if (to - from > 64) continue;
         double s = 0.;
         for (uint32_t i = from + (lane & 15); i < to; i += 16) s += sSlot[i];
-#pragma unroll
-        for (int d = 8; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
-        if ((lane & 15) == 0) sTensor[t] = s;
+        s = row_sum(s);
+        if ((lane & 15) == 15) sTensor[t] = s;
     }
     for (uint32_t t = threadIdx.x >> 6; t < count; t += kThreads / 64) {
-        const uint32_t from = tab.first[t], to = tab.first[t + 1];
+        const uint32_t from = sFirst[t], to = sFirst[t + 1];
         if (to - from <= 64) continue;
         double s = 0.;
+#pragma unroll 4
         for (uint32_t i = from + lane; i < to; i += 64) s += sSlot[i];
         s = wave_sum(s);
         if (lane == 0) sTensor[t] = s;
@@ -221,7 +234,7 @@ __device__ __forceinline__ float finish(const GradTable& tab, const GradEnd& end
     return sScale;
 }
 
-__global__ __launch_bounds__(1024) void k_grad_finish(GradTable tab, GradEnd end)
+__global__ __launch_bounds__(1024) void k_grad_finish(GradEnd end, GradTable tab)
 {
     finish<1024, kGradSlots, false>(tab, end, true);
 }
@@ -229,11 +242,11 @@ __global__ __launch_bounds__(1024) void k_grad_finish(GradTable tab, GradEnd end
 // Every workgroup sums its part into a slot. kAlone: the last one to be done finishes in the same launch: slots go past the
 // caches of the eight dies (agent scope), and the counter is left at zero for the next launch.
 template <bool kAlone>
-__global__ __launch_bounds__(kGradBlock, 8) void k_grad_squares(GradTable tab, GradEnd end)
+__global__ __launch_bounds__(kGradBlock, 8) void k_grad_squares(GradEnd end, GradTable tab)
 {
     __shared__ double sWave[kGradBlock / 64];
     __shared__ bool sLast;
-    if (!kAlone || tab.first[tab.count]) {      // else one workgroup has come to write the norm of nothing
+    if (!kAlone || tab.blocks) {      // else one workgroup has come to write the norm of nothing
         const uint32_t ti = find_tensor(tab, blockIdx.x);
         const GradTensorDev& t = tab.t[ti];
         const uint32_t first = blockIdx.x - tab.first[ti], step = tab.first[ti + 1] - tab.first[ti];
@@ -290,8 +303,8 @@ __device__ void write_scaled(const GradTensorDev& t, float scale, uint32_t first
         constexpr uint32_t kUnit = kGradBlock * kN * kDenseVecs;
         for (uint32_t u = first; u < t.units; u += step) {
             const uint64_t base = (uint64_t)u * kUnit + threadIdx.x * kN;
+            Vec v[kDenseVecs];
             if ((uint64_t)(u + 1) * kUnit <= count) {
-                Vec v[kDenseVecs];
 #pragma unroll
                 for (int j = 0; j < kDenseVecs; ++j) v[j] = *reinterpret_cast<const Vec*>(data + base + j * kGradBlock * kN);
 #pragma unroll
@@ -301,8 +314,13 @@ __device__ void write_scaled(const GradTensorDev& t, float scale, uint32_t first
                     store_vec(v[j], out + base + j * kGradBlock * kN);
                 }
             } else {
+#pragma unroll
+                for (int j = 0; j < kDenseVecs; ++j) v[j] = load_end(data, base + j * kGradBlock * kN, count);
+#pragma unroll
                 for (int j = 0; j < kDenseVecs; ++j)
-                    for (uint64_t i = base + j * kGradBlock * kN, end = min(i + kN, count); i < end; ++i) out[i] = scaled(data[i], scale);
+#pragma unroll
+                    for (int k = 0; k < kN; ++k)
+                        if (base + j * kGradBlock * kN + k < count) out[base + j * kGradBlock * kN + k] = scaled((T)v[j][k], scale);
             }
         }
     } else {
@@ -333,11 +351,15 @@ __device__ void write_scaled(const GradTensorDev& t, float scale, uint32_t first
                         store_vec(v[j], out + o + (uint64_t)j * t.n);
                     }
             } else {
-                for (uint32_t p = w.p0; p < w.p1; ++p)
-                    for (int k = 0; k < kN; ++k) {
-                        const uint64_t a = (uint64_t)p * t.n + w.at + k;
-                        if (used<kN>(mask, k)) out[a] = scaled(data[a], scale);
-                    }
+                Vec v[kMaskPlanes];
+#pragma unroll
+                for (uint32_t j = 0; j < kMaskPlanes; ++j)
+                    if (w.p0 + j < w.p1) v[j] = load_end(data + (uint64_t)(w.p0 + j) * t.n, w.at, t.n);
+#pragma unroll
+                for (uint32_t j = 0; j < kMaskPlanes; ++j)
+#pragma unroll
+                    for (int k = 0; k < kN; ++k)
+                        if (w.p0 + j < w.p1 && used<kN>(mask, k)) out[o + (uint64_t)j * t.n + k] = scaled((T)v[j][k], scale);
             }
         }
     }
@@ -345,7 +367,7 @@ __device__ void write_scaled(const GradTensorDev& t, float scale, uint32_t first
 
 // kFinish: every workgroup adds the slots up for itself, one writes the result: for small lists, whose sums then need no ending
 template <bool kFinish>
-__global__ __launch_bounds__(kGradBlock) void k_grad_scale(GradTable tab, GradEnd end)
+__global__ __launch_bounds__(kGradBlock, 8) void k_grad_scale(GradEnd end, GradTable tab)
 {
     const uint32_t block = gridDim.x - 1 - blockIdx.x;      // backwards: the end of the gradient was read last
     const uint32_t ti = find_tensor(tab, block);
@@ -358,16 +380,8 @@ __global__ __launch_bounds__(kGradBlock) void k_grad_scale(GradTable tab, GradEn
     else write_scaled<kGradBF16>(t, scale, first, step);
 }
 
-// one used entry: Adam with the clipped gradient, g * scale rounded to fp32 as a clipped gradient in memory would be
-__device__ __forceinline__ void adam_clipped(const AdamDev& c, float scale, float* p, float* g, float* m, float* v)
-{
-    float x = *p, mm = *m, vv = *v;
-    adam_one(c, x, scaled(*g, scale), mm, vv);
-    *p = x; *m = mm; *v = vv;
-    if (c.zero_grad) *g = 0.f;
-}
-
-// four entries, of which those with a zero in the mask get their own bits back
+// Four entries: Adam with the clipped gradient, g * scale rounded to fp32 as a clipped gradient in memory would be. Those with a
+// zero in the mask keep their bits.
 struct AdamVec {
     GradVec<float>::V p, g, m, v;
 };
@@ -378,9 +392,12 @@ __device__ __forceinline__ AdamVec adam_load(const AdamTensorDev& t, uint64_t at
     return AdamVec{__builtin_nontemporal_load(reinterpret_cast<const Vec*>(t.param + at)), *reinterpret_cast<const Vec*>(t.grad + at),
                    __builtin_nontemporal_load(reinterpret_cast<const Vec*>(t.m + at)), __builtin_nontemporal_load(reinterpret_cast<const Vec*>(t.v + at))};
 }
-__device__ __forceinline__ void adam_store(const AdamDev& c, float scale, uint32_t mask, const AdamTensorDev& t, uint64_t at, AdamVec x)
+__device__ __forceinline__ AdamVec adam_load_end(const AdamTensorDev& t, uint64_t row, uint64_t at, uint64_t n)
 {
-    using Vec = GradVec<float>::V;
+    return AdamVec{load_end(t.param + row, at, n), load_end(t.grad + row, at, n), load_end(t.m + row, at, n), load_end(t.v + row, at, n)};
+}
+__device__ __forceinline__ void adam_step(const AdamDev& c, float scale, uint32_t mask, AdamVec& x)
+{
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         float a = x.p[k], b = x.m[k], d = x.v[k];
@@ -389,10 +406,23 @@ __device__ __forceinline__ void adam_store(const AdamDev& c, float scale, uint32
             x.p[k] = a; x.m[k] = b; x.v[k] = d; x.g[k] = 0.f;
         }
     }
+}
+__device__ __forceinline__ void adam_store(const AdamDev& c, const AdamTensorDev& t, uint64_t at, const AdamVec& x)
+{
+    using Vec = GradVec<float>::V;
     __builtin_nontemporal_store(x.p, reinterpret_cast<Vec*>(t.param + at));
     __builtin_nontemporal_store(x.m, reinterpret_cast<Vec*>(t.m + at));
     __builtin_nontemporal_store(x.v, reinterpret_cast<Vec*>(t.v + at));
     if (c.zero_grad) *reinterpret_cast<Vec*>(t.grad + at) = x.g;
+}
+__device__ __forceinline__ void adam_store_some(const AdamDev& c, uint32_t mask, const AdamTensorDev& t, uint64_t at, const AdamVec& x)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (used<4>(mask, k)) {
+            t.param[at + k] = x.p[k]; t.m[at + k] = x.m[k]; t.v[at + k] = x.v[k];
+            if (c.zero_grad) t.grad[at + k] = 0.f;
+        }
 }
 
 __global__ __launch_bounds__(kGradBlock) void k_adam_list(AdamTable tab, const float* __restrict__ result)
@@ -408,28 +438,43 @@ __global__ __launch_bounds__(kGradBlock) void k_adam_list(AdamTable tab, const f
         const uint64_t count = t.n * t.planes;
         for (uint32_t u = first; u < t.units; u += step) {
             const uint64_t at = ((uint64_t)u * kGradBlock + threadIdx.x) * 4;
-            if (at + 4 <= count) adam_store(c, scale, ~0u, t, at, adam_load(t, at));
-            else
-                for (uint64_t i = at; i < count; ++i) adam_clipped(c, scale, t.param + i, t.grad + i, t.m + i, t.v + i);
+            if (at + 4 <= count) {
+                AdamVec x = adam_load(t, at);
+                adam_step(c, scale, ~0u, x);
+                adam_store(c, t, at, x);
+            } else if (at < count) {
+                AdamVec x = adam_load_end(t, 0, at, count);
+                adam_step(c, scale, ~0u, x);
+                adam_store_some(c, ~0u >> (8 * (4 - (count - at))), t, at, x);
+            }
         }
     } else {
         for (uint32_t u = first; u < t.units; u += step) {
             const MaskedUnit w = masked_unit<4, kAdamPlanes>(u, t.planes);
             const uint32_t mask = mask_bytes<4>(t.visible, w.at, t.n);
             if (mask == 0) continue;
-            uint64_t at = (uint64_t)w.p0 * t.n + w.at;
+            const uint64_t row = (uint64_t)w.p0 * t.n;
+            AdamVec x[kAdamPlanes];
             if (w.at + 4 <= t.n) {
-                AdamVec x[kAdamPlanes];
 #pragma unroll
                 for (uint32_t j = 0; j < kAdamPlanes; ++j)
-                    if (w.p0 + j < w.p1) x[j] = adam_load(t, at + j * t.n);
+                    if (w.p0 + j < w.p1) x[j] = adam_load(t, row + j * t.n + w.at);
 #pragma unroll
                 for (uint32_t j = 0; j < kAdamPlanes; ++j)
-                    if (w.p0 + j < w.p1) adam_store(c, scale, mask, t, at + j * t.n, x[j]);
+                    if (w.p0 + j < w.p1) {
+                        adam_step(c, scale, mask, x[j]);
+                        adam_store(c, t, row + j * t.n + w.at, x[j]);
+                    }
             } else {
-                for (uint32_t p = w.p0; p < w.p1; ++p, at += t.n)
-                    for (int k = 0; k < 4; ++k)
-                        if (used<4>(mask, k)) adam_clipped(c, scale, t.param + at + k, t.grad + at + k, t.m + at + k, t.v + at + k);
+#pragma unroll
+                for (uint32_t j = 0; j < kAdamPlanes; ++j)
+                    if (w.p0 + j < w.p1) x[j] = adam_load_end(t, row + j * t.n, w.at, t.n);
+#pragma unroll
+                for (uint32_t j = 0; j < kAdamPlanes; ++j)
+                    if (w.p0 + j < w.p1) {
+                        adam_step(c, scale, mask, x[j]);
+                        adam_store_some(c, mask, t, row + j * t.n + w.at, x[j]);
+                    }
             }
         }
     }
@@ -458,7 +503,7 @@ static uint32_t cut_blocks(Table& tab, uint64_t units, uint32_t most)
         at += (uint32_t)ceil_div(tab.t[i].units, tab.t[i].visible || each == 1 ? each : 2 * each);
     }
     if (units >= 64) at = (at + 7) & ~7u;
-    tab.first[tab.count] = at;
+    tab.blocks = tab.first[tab.count] = at;
     return at;
 }
 
@@ -492,14 +537,14 @@ hipError_t launch_grad(int count, const GradTensorDev* list, float max_norm, flo
             const GradEnd end{ws, result, result + 2 + at, max_norm, at == 0, at + (int)tab.count == count};
             const dim3 grid(blocks ? blocks : 1), block(kGradBlock);
             if (blocks && blocks <= kInlineSlots && units <= kGradBlocks && clip && end.first_table && end.last_table) {      // a workgroup per unit
-                hipLaunchKernelGGL(k_grad_squares<false>, grid, block, 0, s, tab, end);
-                hipLaunchKernelGGL(k_grad_scale<true>, grid, block, 0, s, tab, end);
+                hipLaunchKernelGGL(k_grad_squares<false>, grid, block, 0, s, end, tab);
+                hipLaunchKernelGGL(k_grad_scale<true>, grid, block, 0, s, end, tab);
                 scaled = true;
             } else if (blocks <= kAloneSlots) {
-                hipLaunchKernelGGL(k_grad_squares<true>, grid, block, 0, s, tab, end);
+                hipLaunchKernelGGL(k_grad_squares<true>, grid, block, 0, s, end, tab);
             } else {
-                hipLaunchKernelGGL(k_grad_squares<false>, grid, block, 0, s, tab, end);
-                hipLaunchKernelGGL(k_grad_finish, dim3(1), dim3(1024), 0, s, tab, end);
+                hipLaunchKernelGGL(k_grad_squares<false>, grid, block, 0, s, end, tab);
+                hipLaunchKernelGGL(k_grad_finish, dim3(1), dim3(1024), 0, s, end, tab);
             }
             at += (int)tab.count;
         } while (at < count);
@@ -510,7 +555,7 @@ hipError_t launch_grad(int count, const GradTensorDev* list, float max_norm, flo
             const uint64_t units = fill_table(tab, list + at, count - at);
             const uint32_t blocks = cut_blocks(tab, units, kMostBlocks);
             const GradEnd end{ws, result, result + 2 + at, max_norm, 0, 0};
-            if (blocks) hipLaunchKernelGGL(k_grad_scale<false>, dim3(blocks), dim3(kGradBlock), 0, s, tab, end);
+            if (blocks) hipLaunchKernelGGL(k_grad_scale<false>, dim3(blocks), dim3(kGradBlock), 0, s, end, tab);
         }
     }
     return hipGetLastError();
