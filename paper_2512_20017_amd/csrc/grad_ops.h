@@ -9,14 +9,15 @@ enum { kGradF32 = 0, kGradF16 = 1, kGradBF16 = 2 };
 constexpr int kGradBlock = 256;
 constexpr int kDenseVecs = 2;                     // vectors of a lane in a unit of a tensor without mask (2, 4, 8: the same within 2 %)
 // Planes of a masked unit, all of which are read before the first is used. Sums and scaling: 4 (8M points, a quarter used: norm
-// 100 us, clipped into buffers of their own 401; 6 planes 114 and 420; 8 planes 98 and 425). Adam reads four vectors a plane: 3
-// (with the norm 753 us; 1: 766, 2: 751, 4: 757, 6: 790; 1M points: 212, 211, 213, 213, 217); attributes have 1, 2, 3, 4 or 3K planes.
+// 97 us, clipped into buffers of their own 386; 8 planes 98 and 425, 6 between). Adam reads four vectors a plane: 2 (8M points, a
+// quarter used, with the norm: 736 us; 1 plane 766, 3 planes 740, 4 750; 1M points 207 each; 200,003 surfels 56, 3 and 4 planes 57).
 constexpr uint32_t kMaskPlanes = 4;
-constexpr uint32_t kAdamPlanes = 3;
+constexpr uint32_t kAdamPlanes = 2;
 // Workgroups of a launch that sums or scales, eight per compute unit: units that need no reading leave gaps in masked tensors
 // (8M points, a quarter used: norm 99 us; 1,024 workgroups 113, 512 168; 4,096 103). Tensors without mask take half as many
 // for their units, and stream better so (2M surfels clipped: 239 us against 251).
 constexpr uint32_t kGradBlocks = 2048;
+constexpr uint32_t kLineFloats = 32;              // of a cache line
 constexpr uint32_t kMostBlocks = 1u << 23;        // of a launch: fewer than 2^32 threads
 constexpr int kGradTableTensors = 88;             // tensors of one launch: the table is a kernel argument, of 4 KB at most
 constexpr int kAdamTableTensors = 48;
@@ -50,9 +51,8 @@ struct AdamTable {
     AdamTensorDev t[kAdamTableTensors];
 };
 
-// a slot per workgroup that sums: a table's workgroups are kGradBlocks, one more per tensor where its units do not come out even,
-// and up to seven before each tensor and at the end for the dies' sake
-constexpr uint32_t kGradSlots = kGradBlocks + 8 * (kGradTableTensors + 1);
+// a slot per workgroup that sums: a table has kGradBlocks of them at most, and one more per tensor whose units do not come out even
+constexpr uint32_t kGradSlots = kGradBlocks + kGradTableTensors;
 // Workgroups up to which one launch sums and finishes: 32 to 128 workgroups 8.3 us a call, 11 with a launch of its own for the
 // end; 250 workgroups 10.5 and 10.3; 500 15.3 and 10.5.
 constexpr uint32_t kAloneSlots = 128;

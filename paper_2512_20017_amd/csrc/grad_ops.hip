@@ -70,19 +70,18 @@ struct MaskedUnit {
     uint64_t at;
     uint32_t p0, p1;
 };
-template <int kN, uint32_t kPlanes>
+template <int kN>
 __device__ __forceinline__ MaskedUnit masked_unit(uint32_t u, uint32_t planes)
 {
-    const uint32_t groups = (planes + kPlanes - 1) / kPlanes, eight = u / (8 * groups), in8 = u - eight * 8 * groups;
-    const uint32_t seg = eight * 8 + (in8 & 7), p0 = (in8 >> 3) * kPlanes;
-    return MaskedUnit{((uint64_t)seg * kGradBlock + threadIdx.x) * kN, p0, min(p0 + kPlanes, planes)};
+    const uint32_t groups = (planes + kMaskPlanes - 1) / kMaskPlanes, seg = u / groups, p0 = (u - seg * groups) * kMaskPlanes;
+    return MaskedUnit{((uint64_t)seg * kGradBlock + threadIdx.x) * kN, p0, min(p0 + kMaskPlanes, planes)};
 }
 
 template <int kN>
 __device__ __forceinline__ typename MaskOf<kN>::T unit_mask(const GradTensorDev& t, uint32_t u)
 {
     if (u >= t.units) return 0;
-    return mask_bytes<kN>(t.visible, masked_unit<kN, kMaskPlanes>(u, t.planes).at, t.n);
+    return mask_bytes<kN>(t.visible, masked_unit<kN>(u, t.planes).at, t.n);
 }
 
 template <class T>
@@ -124,7 +123,7 @@ __device__ double sum_squares(const GradTensorDev& t, uint32_t first, uint32_t s
             const typename MaskOf<kN>::T mask = next;
             next = unit_mask<kN>(t, u + step);      // on its way while this unit's values are
             if (mask == 0) continue;
-            const MaskedUnit w = masked_unit<kN, kMaskPlanes>(u, t.planes);
+            const MaskedUnit w = masked_unit<kN>(u, t.planes);
             const T* row = data + (uint64_t)w.p0 * t.n;
             Vec v[kMaskPlanes];
             if (w.at + kN <= t.n) {
@@ -325,7 +324,7 @@ __device__ void write_scaled(const GradTensorDev& t, float scale, uint32_t first
         }
     } else {
         for (uint32_t u = first; u < t.units; u += step) {
-            const MaskedUnit w = masked_unit<kN, kMaskPlanes>(u, t.planes);
+            const MaskedUnit w = masked_unit<kN>(u, t.planes);
             const typename MaskOf<kN>::T mask = mask_bytes<kN>(t.visible, w.at, t.n);
             if (mask == 0) continue;
             const uint64_t o = (uint64_t)w.p0 * t.n + w.at;
@@ -380,22 +379,47 @@ __global__ __launch_bounds__(kGradBlock, 8) void k_grad_scale(GradEnd end, GradT
     else write_scaled<kGradBF16>(t, scale, first, step);
 }
 
-// Four entries: Adam with the clipped gradient, g * scale rounded to fp32 as a clipped gradient in memory would be. Those with a
-// zero in the mask keep their bits.
+// Adam. A lane takes four entries of a row, and a workgroup's stretch of a row begins on a cache line of the moments, wherever the
+// row begins: lines that two wavefronts write in part cost 12 % of the whole (200,003 points 64 us, 200,000 points 57). So lanes
+// may stand before the row's begin, and the mask is read at the plane's own offset. Of parameter, gradient and moments the
+// vectors lie on 16 bytes each.
 struct AdamVec {
     GradVec<float>::V p, g, m, v;
 };
-__device__ __forceinline__ AdamVec adam_load(const AdamTensorDev& t, uint64_t at)
+
+// the bytes of the mask of four points from `at` on, or ones without a mask; zero outside the row
+template <bool kMasked>
+__device__ __forceinline__ uint32_t adam_mask(const uint8_t* __restrict__ visible, int64_t at, int64_t n)
+{
+    struct __attribute__((packed)) Any { uint32_t bytes; };
+    if (at >= 0 && at + 4 <= n) return kMasked ? reinterpret_cast<const Any*>(visible + at)->bytes : ~0u;
+    if (at >= n || at <= -4) return 0;
+    uint8_t byte[4] = {1, 1, 1, 1};
+    if (kMasked) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) byte[k] = visible[max((int64_t)0, min(at + k, n - 1))];
+    }
+    uint32_t m = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) m |= at + k >= 0 && at + k < n ? (uint32_t)byte[k] << (8 * k) : 0u;
+    return m;
+}
+__device__ __forceinline__ GradVec<float>::V load_near(const float* row, int64_t at, int64_t n)      // at an end of the row
+{
+    GradVec<float>::V v;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = row[max((int64_t)0, min(at + k, n - 1))];
+    return v;
+}
+__device__ __forceinline__ AdamVec adam_load(const AdamTensorDev& t, uint64_t row, int64_t at, int64_t n)
 {
     using Vec = GradVec<float>::V;
+    if (at < 0 || at + 4 > n) return AdamVec{load_near(t.param + row, at, n), load_near(t.grad + row, at, n), load_near(t.m + row, at, n), load_near(t.v + row, at, n)};
     // parameters and moments pass by the last-level cache, which holds part of the gradient that the norm has just read
-    return AdamVec{__builtin_nontemporal_load(reinterpret_cast<const Vec*>(t.param + at)), *reinterpret_cast<const Vec*>(t.grad + at),
-                   __builtin_nontemporal_load(reinterpret_cast<const Vec*>(t.m + at)), __builtin_nontemporal_load(reinterpret_cast<const Vec*>(t.v + at))};
+    return AdamVec{__builtin_nontemporal_load(reinterpret_cast<const Vec*>(t.param + row + at)), *reinterpret_cast<const Vec*>(t.grad + row + at),
+                   __builtin_nontemporal_load(reinterpret_cast<const Vec*>(t.m + row + at)), __builtin_nontemporal_load(reinterpret_cast<const Vec*>(t.v + row + at))};
 }
-__device__ __forceinline__ AdamVec adam_load_end(const AdamTensorDev& t, uint64_t row, uint64_t at, uint64_t n)
-{
-    return AdamVec{load_end(t.param + row, at, n), load_end(t.grad + row, at, n), load_end(t.m + row, at, n), load_end(t.v + row, at, n)};
-}
+// g * scale is rounded to fp32 as a clipped gradient in memory would be; entries with a zero in the mask keep their bits
 __device__ __forceinline__ void adam_step(const AdamDev& c, float scale, uint32_t mask, AdamVec& x)
 {
 #pragma unroll
@@ -407,22 +431,55 @@ __device__ __forceinline__ void adam_step(const AdamDev& c, float scale, uint32_
         }
     }
 }
-__device__ __forceinline__ void adam_store(const AdamDev& c, const AdamTensorDev& t, uint64_t at, const AdamVec& x)
+__device__ __forceinline__ void adam_store(const AdamDev& c, uint32_t mask, const AdamTensorDev& t, uint64_t row, int64_t at, int64_t n, const AdamVec& x)
 {
     using Vec = GradVec<float>::V;
-    __builtin_nontemporal_store(x.p, reinterpret_cast<Vec*>(t.param + at));
-    __builtin_nontemporal_store(x.m, reinterpret_cast<Vec*>(t.m + at));
-    __builtin_nontemporal_store(x.v, reinterpret_cast<Vec*>(t.v + at));
-    if (c.zero_grad) *reinterpret_cast<Vec*>(t.grad + at) = x.g;
-}
-__device__ __forceinline__ void adam_store_some(const AdamDev& c, uint32_t mask, const AdamTensorDev& t, uint64_t at, const AdamVec& x)
-{
+    if (at >= 0 && at + 4 <= n) {
+        __builtin_nontemporal_store(x.p, reinterpret_cast<Vec*>(t.param + row + at));
+        __builtin_nontemporal_store(x.m, reinterpret_cast<Vec*>(t.m + row + at));
+        __builtin_nontemporal_store(x.v, reinterpret_cast<Vec*>(t.v + row + at));
+        if (c.zero_grad) *reinterpret_cast<Vec*>(t.grad + row + at) = x.g;
+    } else {
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (used<4>(mask, k)) {
-            t.param[at + k] = x.p[k]; t.m[at + k] = x.m[k]; t.v[at + k] = x.v[k];
-            if (c.zero_grad) t.grad[at + k] = 0.f;
+        for (int k = 0; k < 4; ++k)
+            if (used<4>(mask, k)) {
+                const uint64_t i = row + at + k;
+                t.param[i] = x.p[k]; t.m[i] = x.m[k]; t.v[i] = x.v[k];
+                if (c.zero_grad) t.grad[i] = 0.f;
+            }
+    }
+}
+
+// without a mask the tensor is one row
+template <bool kMasked>
+__device__ __forceinline__ void adam_tensor(const AdamTensorDev& t, const AdamDev& c, float scale, uint32_t first, uint32_t step)
+{
+    constexpr uint32_t kPlanes = kMasked ? kAdamPlanes : 1;
+    const uint32_t rows = kMasked ? t.planes : 1, groups = (rows + kPlanes - 1) / kPlanes;
+    const int64_t n = (int64_t)(kMasked ? t.n : t.n * t.planes);
+    for (uint32_t u = first; u < t.units; u += step) {
+        const uint32_t seg = u / groups, p0 = (u - seg * groups) * kPlanes;
+        int64_t at[kPlanes];
+        uint32_t mask[kPlanes], any = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < kPlanes; ++j) {
+            const uint64_t row = (uint64_t)(p0 + j) * n;
+            at[j] = ((int64_t)seg * kGradBlock + threadIdx.x) * 4 - (int64_t)((reinterpret_cast<uintptr_t>(t.m + row) >> 2) & (kLineFloats - 1));
+            mask[j] = p0 + j < rows ? adam_mask<kMasked>(t.visible, at[j], n) : 0u;
+            any |= mask[j];
         }
+        if (any == 0) continue;
+        AdamVec x[kPlanes];
+#pragma unroll
+        for (uint32_t j = 0; j < kPlanes; ++j)
+            if (mask[j]) x[j] = adam_load(t, (uint64_t)(p0 + j) * n, at[j], n);
+#pragma unroll
+        for (uint32_t j = 0; j < kPlanes; ++j)
+            if (mask[j]) {
+                adam_step(c, scale, mask[j], x[j]);
+                adam_store(c, mask[j], t, (uint64_t)(p0 + j) * n, at[j], n, x[j]);
+            }
+    }
 }
 
 __global__ __launch_bounds__(kGradBlock) void k_adam_list(AdamTable tab, const float* __restrict__ result)
@@ -434,61 +491,24 @@ __global__ __launch_bounds__(kGradBlock) void k_adam_list(AdamTable tab, const f
     AdamDev c = tab.adam;
     c.step_size = t.step_size;
     const uint32_t first = block - tab.first[ti], step = tab.first[ti + 1] - tab.first[ti];
-    if (t.visible == nullptr) {
-        const uint64_t count = t.n * t.planes;
-        for (uint32_t u = first; u < t.units; u += step) {
-            const uint64_t at = ((uint64_t)u * kGradBlock + threadIdx.x) * 4;
-            if (at + 4 <= count) {
-                AdamVec x = adam_load(t, at);
-                adam_step(c, scale, ~0u, x);
-                adam_store(c, t, at, x);
-            } else if (at < count) {
-                AdamVec x = adam_load_end(t, 0, at, count);
-                adam_step(c, scale, ~0u, x);
-                adam_store_some(c, ~0u >> (8 * (4 - (count - at))), t, at, x);
-            }
-        }
-    } else {
-        for (uint32_t u = first; u < t.units; u += step) {
-            const MaskedUnit w = masked_unit<4, kAdamPlanes>(u, t.planes);
-            const uint32_t mask = mask_bytes<4>(t.visible, w.at, t.n);
-            if (mask == 0) continue;
-            const uint64_t row = (uint64_t)w.p0 * t.n;
-            AdamVec x[kAdamPlanes];
-            if (w.at + 4 <= t.n) {
-#pragma unroll
-                for (uint32_t j = 0; j < kAdamPlanes; ++j)
-                    if (w.p0 + j < w.p1) x[j] = adam_load(t, row + j * t.n + w.at);
-#pragma unroll
-                for (uint32_t j = 0; j < kAdamPlanes; ++j)
-                    if (w.p0 + j < w.p1) {
-                        adam_step(c, scale, mask, x[j]);
-                        adam_store(c, t, row + j * t.n + w.at, x[j]);
-                    }
-            } else {
-#pragma unroll
-                for (uint32_t j = 0; j < kAdamPlanes; ++j)
-                    if (w.p0 + j < w.p1) x[j] = adam_load_end(t, row + j * t.n, w.at, t.n);
-#pragma unroll
-                for (uint32_t j = 0; j < kAdamPlanes; ++j)
-                    if (w.p0 + j < w.p1) {
-                        adam_step(c, scale, mask, x[j]);
-                        adam_store_some(c, mask, t, row + j * t.n + w.at, x[j]);
-                    }
-            }
-        }
-    }
+    if (t.visible) adam_tensor<true>(t, c, scale, first, step);
+    else adam_tensor<false>(t, c, scale, first, step);
 }
 
 static uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
-// units of a tensor whose vectors have `vec` values
-template <class T>
-static void cut_units(T& t, uint64_t vec, uint64_t dense_vecs, uint32_t planes)
+static uint32_t units_of(const GradTensorDev& t)
 {
-    if (t.n == 0 || t.planes == 0) t.units = 0;
-    else if (t.visible == nullptr) t.units = (uint32_t)ceil_div(t.n * t.planes, kGradBlock * vec * dense_vecs);
-    else t.units = (uint32_t)(ceil_div(t.n, kGradBlock * vec * 8) * 8 * ceil_div(t.planes, planes));
+    const uint64_t vec = t.dtype == kGradF32 ? 4 : 8;
+    if (t.n == 0 || t.planes == 0) return 0;
+    if (t.visible == nullptr) return (uint32_t)ceil_div(t.n * t.planes, kGradBlock * vec * kDenseVecs);
+    return (uint32_t)(ceil_div(t.n, kGradBlock * vec) * ceil_div(t.planes, kMaskPlanes));
+}
+static uint32_t units_of(const AdamTensorDev& t)      // lanes may stand before the begin of a row by a line less one
+{
+    if (t.n == 0 || t.planes == 0) return 0;
+    if (t.visible == nullptr) return (uint32_t)ceil_div(t.n * t.planes + kLineFloats - 1, kGradBlock * 4);
+    return (uint32_t)(ceil_div(t.n + kLineFloats - 1, kGradBlock * 4) * ceil_div(t.planes, kAdamPlanes));
 }
 
 // The workgroups of a table: one per unit, or, with more than `most` units, equal runs of them.
@@ -498,11 +518,9 @@ static uint32_t cut_blocks(Table& tab, uint64_t units, uint32_t most)
     const uint64_t each = units > most ? ceil_div(units, most) : 1;
     uint32_t at = 0;
     for (uint32_t i = 0; i < tab.count; ++i) {
-        if (tab.t[i].visible && tab.t[i].units >= 64) at = (at + 7) & ~7u;      // for the dies, see masked_unit()
         tab.first[i] = at;
         at += (uint32_t)ceil_div(tab.t[i].units, tab.t[i].visible || each == 1 ? each : 2 * each);
     }
-    if (units >= 64) at = (at + 7) & ~7u;
     tab.blocks = tab.first[tab.count] = at;
     return at;
 }
@@ -514,8 +532,7 @@ static uint64_t fill_table(GradTable& tab, const GradTensorDev* list, int count)
     tab.count = (uint32_t)(count < kGradTableTensors ? count : kGradTableTensors);
     for (uint32_t i = 0; i < tab.count; ++i) {
         tab.t[i] = list[i];
-        cut_units(tab.t[i], list[i].dtype == kGradF32 ? 4 : 8, kDenseVecs, kMaskPlanes);
-        units += tab.t[i].units;
+        units += tab.t[i].units = units_of(list[i]);
     }
     return units;
 }
@@ -571,8 +588,7 @@ hipError_t launch_adam_list(int count, const AdamTensorDev* list, const AdamDev&
         tab.count = (uint32_t)(count - at < kAdamTableTensors ? count - at : kAdamTableTensors);
         for (uint32_t i = 0; i < tab.count; ++i) {
             tab.t[i] = list[at + i];
-            cut_units(tab.t[i], 4, 1, kAdamPlanes);
-            units += tab.t[i].units;
+            units += tab.t[i].units = units_of(tab.t[i]);
         }
         const uint32_t blocks = cut_blocks(tab, units, kMostBlocks);
         if (blocks) hipLaunchKernelGGL(k_adam_list, dim3(blocks), dim3(kGradBlock), 0, s, tab, result);
