@@ -303,6 +303,107 @@ def test_refusals_on_the_gpu():
     assert (t == 1).all()
 
 
+@pytest.mark.parametrize("n", [1, 3, 31, 33, 1023, 1025, 2050, 40_003])
+@pytest.mark.parametrize("masked", [True, False])
+def test_rows_and_buffers_that_begin_anywhere_on_a_line(n, masked):
+    """Parameter, gradient, moments and output each at another multiple of 16 bytes, rows at any multiple of a value: what lies
+    before, between and behind keeps its bits, unused entries too (NaN with a payload, infinities)."""
+    rng = np.random.default_rng(n)
+    planes = 5
+    mask = torch.from_numpy((rng.uniform(size=n) < 0.8).astype(np.uint8)).cuda() if masked else None
+    used = torch.ones(n, dtype=torch.bool, device="cuda") if mask is None else mask != 0
+    guard = 0x7FA12345      # a NaN
+
+    def buffer(shift, values):
+        flat = torch.full((planes * n + 64,), guard, dtype=torch.int32, device="cuda").view(F32)
+        view = flat[shift:shift + planes * n].view(planes, n)
+        bits = torch.from_numpy(values.astype(np.float32)).cuda().view(torch.int32)
+        view.view(torch.int32).copy_(torch.where(used, bits, torch.full_like(bits, guard)))
+        return flat, view
+
+    values = [rng.normal(size=(planes, n)), rng.normal(size=(planes, n)) * 1e-3, rng.normal(size=(planes, n)) * 1e-3, rng.uniform(size=(planes, n)) * 1e-6]
+    flats, (p, g, m, v) = zip(*[buffer(shift, x) for shift, x in zip((4, 8, 28, 16), values)])
+    out_flat, out = buffer(12, values[1])
+    before = [f.view(torch.int32).clone() for f in (*flats, out_flat)]
+    result, ws = torch.empty(3, device="cuda"), B.alloc_grad_workspace(1)
+    limit = float(np.float32(reference([g], [mask], np.inf)[0] * 0.5))
+    B.pbdr_grad_clip(B.GradList([g], visible=mask, out=[out]), limit, result, ws)
+    B.pbdr_adam_selective_list(B.AdamList([p], [g], [m], [v], [1e-2], visible=mask), 0.9, 0.999, 1e-15, 3, clip=result, zero_grad=True)
+    # the same on buffers of their own, by pbdr_adam_selective
+    q, h, a, b = (torch.from_numpy(x.astype(np.float32)).cuda() for x in values)
+    h.mul_(result[1])
+    B.pbdr_adam_selective(q, h, a, b, torch.ones(n, dtype=torch.uint8, device="cuda") if mask is None else mask, 1e-2, 0.9, 0.999, 1e-15, 3)
+    torch.cuda.synchronize()
+    for got, want, name in ((p, q, "p"), (m, a, "m"), (v, b, "v"), (out, h, "out"), (g, torch.zeros_like(h), "g")):
+        assert torch.equal(got[:, used], want[:, used]), name
+    for flat, old, view in zip((*flats, out_flat), before, (p, g, m, v, out)):
+        changed = flat.view(torch.int32) != old
+        start = (view.data_ptr() - flat.data_ptr()) // 4
+        inside = torch.zeros_like(changed)
+        inside[start:start + planes * n] = used.repeat(planes)
+        assert not (changed & ~inside).any()
+
+
+def test_two_graphs_share_a_workspace_and_streams_change():
+    """Every form of the sum's end (in the launch, in the scaling, in a launch of its own, over two tables), recorded twice with
+    one workspace, replayed in turn with eager calls between, against the eager results; and the eager calls on another stream."""
+    specs = [[((3, 900), F32, 0.5), ((64,), BF16, None)], [((14, 30_000), F32, None)], [((48, 30_001), F32, 0.6), ((3, 30_001), F32, 0.6)],
+             [((int(k % 7) * 100 + 1,), (F32, F16)[k % 2], None) for k in range(120)]]
+    ws = B.alloc_grad_workspace(120)
+    for k, spec in enumerate(specs):
+        ts, ms = make(spec, k)
+        limit = float(np.float32(reference(ts, ms, np.inf)[0] * 0.5))
+        adam = [i for i, t in enumerate(ts) if t.dtype == F32]
+        def state():
+            g = [t.clone() for t in ts]
+            p, m, v = ([torch.zeros_like(ts[i]) for i in adam] for _ in range(3))
+            s = dict(g=g, out=[torch.zeros_like(t) for t in ts], p=p, m=m, v=v, result=torch.zeros(2 + len(ts), device="cuda"), clip=torch.zeros(2 + len(ts), device="cuda"))
+            s["norm"], s["to"] = B.GradList(g, visible=ms), B.GradList(g, visible=ms, out=s["out"])
+            s["adam"] = B.AdamList(p, [g[i] for i in adam], m, v, [1e-3] * len(adam), visible=[ms[i] for i in adam])
+            return s
+
+        def run(s, stream=None):
+            B.pbdr_grad_norm(s["norm"], limit, s["result"], ws, stream=stream)
+            B.pbdr_grad_clip(s["to"], limit, s["clip"], ws, stream=stream)
+            B.pbdr_adam_selective_list(s["adam"], 0.9, 0.999, 1e-15, 2, clip=s["result"], stream=stream)
+
+        def flat(s):
+            return [x.view(torch.int32 if x.dtype == F32 else torch.int16) for x in (s["result"], s["clip"], *s["out"], *s["p"], *s["m"], *s["v"])]
+
+        states, graphs = [state(), state()], []
+        ref = state()
+        run(state())
+        torch.cuda.synchronize()
+        for s in states:
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1]):
+                run(s)
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        for rep in range(3):
+            for graph in graphs:
+                graph.replay()
+            torch.cuda.synchronize()
+            run(ref, stream=side if rep == 1 else None)
+            torch.cuda.synchronize()
+            assert 0 < float(ref["result"][1]) < 1
+            for s in states:
+                assert all(torch.equal(a, b) for a, b in zip(flat(s), flat(ref))), (k, rep)
+
+
+def test_lists_follow_tensors_that_get_other_memory():
+    t, mask = torch.ones(3, 50, device="cuda"), torch.ones(50, dtype=torch.bool, device="cuda")
+    mask[10:] = False
+    gl = B.GradList([t], visible=mask)
+    result, ws = torch.empty(3, device="cuda"), B.alloc_grad_workspace(1)
+    B.pbdr_grad_norm(gl, 1e9, result, ws)
+    assert float(result[0]) == pytest.approx(30 ** 0.5, rel=1e-6)
+    t.data = torch.full((7, 50), 2.0, device="cuda")
+    B.pbdr_grad_clip(gl, 1.0, result, ws)
+    assert float(result[0]) == pytest.approx((7 * 10 * 4) ** 0.5, rel=1e-6)
+    assert float(t[:, :10].norm()) == pytest.approx(1.0, rel=1e-6) and (t[:, 10:] == 2).all()
+
+
 # ------------------------------------------------------------------------------------------------------- a training iteration
 def test_a_training_iteration_eager_and_replayed():
     """Render, loss, backward, norm over the scene and a small network's 16-bit gradients, Adam with the factor: recorded
