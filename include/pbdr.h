@@ -417,14 +417,14 @@ int pbdr_preprocess_bwd_batch_adam(const pbdr_scene* scene, int32_t num_views, c
                                    const float lr[5], const pbdr_adam_config* cfg, void* hip_stream);
 
 /* ------------------------------------------------------------------------------------------------------------
- * Between backward and update (Alg. 1 line 26 names nothing there): the norm of the gradient over all tensors of a
+ * Between backward and update (where the paper has nothing; an addition of this library): the norm of the gradient over all tensors of a
  * model, its clipping, and the selective Adam step over a list of tensors that takes the clipping factor from the device.
  *
  * A list is a HOST array of num_tensors in [0, PBDR_MAX_GRAD_TENSORS] structs; the pointers inside them are device
  * pointers. A tensor is [planes][n] without gaps; n or planes may be 0 (its pointers are then not looked at). An entry is
- * USED if visible is NULL or visible[i] != 0 for its point i; entries that are not used are neither counted nor written,
- * whatever they hold. Gradients of other learned things may be in the same list (planes = 1, visible = NULL), in 16 bits
- * too.
+ * USED if visible is NULL or visible[i] != 0 for its point i; entries that are not used are not counted, whatever they
+ * hold, and keep their bits (one between used ones may be read and written back). Gradients of other learned things may
+ * be in the same list (planes = 1, visible = NULL), in 16 bits too.
  *
  * pbdr_grad_norm writes result (device, float [2 + num_tensors]):
  *   result[0]     = norm  = sqrt(sum of g^2 over the used entries of all tensors)

@@ -297,6 +297,7 @@ __device__ void write_scaled(const GradTensorDev& t, float scale, uint32_t first
     constexpr int kN = GradVec<T>::kN;
     const T* data = static_cast<const T*>(t.data);      // may be the output
     T* out = static_cast<T*>(t.out);
+    const bool apart = out != data;
     const uint64_t count = t.n * t.planes;
     if (t.visible == nullptr) {
         constexpr uint32_t kUnit = kGradBlock * kN * kDenseVecs;
@@ -332,12 +333,12 @@ __device__ void write_scaled(const GradTensorDev& t, float scale, uint32_t first
                 bool all = true;
 #pragma unroll
                 for (int k = 0; k < kN; ++k) all = all && used<kN>(mask, k);
-                Vec v[kMaskPlanes], old[kMaskPlanes];
+                Vec v[kMaskPlanes], old[kMaskPlanes] = {};      // old: of the lanes that need it, on its way together with v
 #pragma unroll
                 for (uint32_t j = 0; j < kMaskPlanes; ++j)
-                    if (w.p0 + j < w.p1) old[j] = v[j] = *reinterpret_cast<const Vec*>(data + o + (uint64_t)j * t.n);
+                    if (w.p0 + j < w.p1) v[j] = *reinterpret_cast<const Vec*>(data + o + (uint64_t)j * t.n);
                 // an unused entry among used ones is read and written back: stores that leave holes in a line cost the memory more
-                if (!all && out != data) {
+                if (!all && apart) {
 #pragma unroll
                     for (uint32_t j = 0; j < kMaskPlanes; ++j)
                         if (w.p0 + j < w.p1) old[j] = *reinterpret_cast<const Vec*>(out + o + (uint64_t)j * t.n);
@@ -346,7 +347,7 @@ __device__ void write_scaled(const GradTensorDev& t, float scale, uint32_t first
                 for (uint32_t j = 0; j < kMaskPlanes; ++j)
                     if (w.p0 + j < w.p1) {
 #pragma unroll
-                        for (int k = 0; k < kN; ++k) v[j][k] = used<kN>(mask, k) ? scaled((T)v[j][k], scale) : (T)old[j][k];
+                        for (int k = 0; k < kN; ++k) v[j][k] = used<kN>(mask, k) ? scaled((T)v[j][k], scale) : apart ? (T)old[j][k] : (T)v[j][k];
                         store_vec(v[j], out + o + (uint64_t)j * t.n);
                     }
             } else {
