@@ -13,9 +13,9 @@ constexpr int kDenseVecs = 2;                     // vectors of a lane in a unit
 // quarter used, with the norm: 736 us; 1 plane 766, 3 planes 740, 4 750; 1M points 207 each; 200,003 surfels 56, 3 and 4 planes 57).
 constexpr uint32_t kMaskPlanes = 4;
 constexpr uint32_t kAdamPlanes = 2;
-// Workgroups of a launch that sums or scales, eight per compute unit: units that need no reading leave gaps in masked tensors
-// (8M points, a quarter used: norm 99 us; 1,024 workgroups 113, 512 168; 4,096 103). Tensors without mask take half as many
-// for their units, and stream better so (2M surfels clipped: 239 us against 251).
+// Workgroups of a launch that sums, eight per compute unit: units that need no reading leave gaps in masked tensors (8M points, a
+// quarter used: norm 99 us; 1,024 workgroups 113, 512 168; 4,096 103). Tensors without mask take half as many for their units, and
+// stream better so (1M points: norm 43.7 us against 45.8).
 constexpr uint32_t kGradBlocks = 2048;
 constexpr uint32_t kLineFloats = 32;              // of a cache line
 constexpr uint32_t kMostBlocks = 1u << 23;        // of a launch: fewer than 2^32 threads

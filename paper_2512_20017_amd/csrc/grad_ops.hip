@@ -389,10 +389,11 @@ __global__ __launch_bounds__(kGradBlock, 8) void k_grad_scale(GradEnd end, GradT
 
 // Adam, a unit per workgroup: 28 bytes an entry, and the gradient's four again. 1M points SH3, 60 % used: 173 us for 0.96 GB beside a
 // gradient that is still cached, 5.5 TB/s; 8M points, a quarter used: 639 us for 3.2 GB and 0.46 GB of gradient, 5.7 TB/s. With
-// ordinary loads and stores of parameters and moments 203 us at 1M points, forwards 680 us at 8M. A lane takes four entries of a row, and a workgroup's stretch of a row begins on a cache line of the moments, wherever the
-// row begins: lines that two wavefronts write in part cost 12 % of the whole (200,003 points 64 us, 200,000 points 57). So lanes
-// may stand before the row's begin, and the mask is read at the plane's own offset. Of parameter, gradient and moments the
-// vectors lie on 16 bytes each.
+// ordinary loads and stores of parameters and moments 203 us at 1M points, forwards 680 us at 8M.
+// A lane takes four entries of a row, and a workgroup's stretch of a row begins on a cache line of the moments, wherever the row
+// begins: lines that two wavefronts write in part cost 12 % of the whole (with the norm 200,003 surfels 64 us, 200,000 surfels 57). So
+// lanes may stand before the row's begin, and the mask is read at the plane's own offset. The vectors of parameter, gradient and
+// moments lie on 16 bytes each.
 struct AdamVec {
     GradVec<float>::V p, g, m, v;
 };

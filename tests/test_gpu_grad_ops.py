@@ -84,7 +84,9 @@ def run_clip(ts, ms, max_norm, in_place=False):
     B.pbdr_grad_norm(B.GradList(raw, visible=ms), max_norm, alone, ws)
     torch.cuda.synchronize()
     assert torch.equal(result.view(torch.int32), alone.view(torch.int32))
-    ref = reference(raw, ms, max_norm)
+    # the boundary takes max_norm as fp32 (1e-3 is 4.7e-8 from its fp32 number, a rounding of the factor allows 6.0e-8): the oracle
+    # gets the same number
+    ref = reference(raw, ms, float(np.float32(max_norm)))
     check_result(result, ref, max_norm)
     for o, b, t, m in zip(ts if in_place else out, before, raw, ms):
         check_clipped(o, b, t, m, ref[1])
@@ -120,7 +122,17 @@ def test_norm_and_clipping(name, share):
     run_clip(ts, ms, float(np.float32(norm * share)), in_place=share == 0.999)
 
 
-@pytest.mark.parametrize("count", [63, 64, 65, 200, 1024])
+@pytest.mark.parametrize("units", [1, 127, 128, 129, 1023, 1024, 1025, 2047, 2048, 2049, 4100])
+@pytest.mark.parametrize("masked", [False, True])
+def test_lengths_at_which_the_sum_ends_another_way(units, masked):
+    """Units are 2,048 values without a mask, 4 planes of 1,024 points with one; a small tensor goes with the large one."""
+    spec = [((4, units * 1024 - 3), F32, 0.5)] if masked else [((units * 2048 - 3,), F32, None)]
+    ts, ms = make(spec + [((5,), F16, None)], units)
+    norm = reference(ts, ms, np.inf)[0]
+    run_clip(ts, ms, float(np.float32(norm * 0.5)), in_place=bool(units & 1))
+
+
+@pytest.mark.parametrize("count", [63, 64, 65, 87, 88, 89, 177, 200, 1024])
 def test_many_tensors(count):
     rng = np.random.default_rng(count)
     spec = [((int(rng.integers(0, 300)),), (F32, F16, BF16)[k % 3], None) if k % 5 else ((3, int(rng.integers(1, 2000))), F32, 0.5) for k in range(count)]
