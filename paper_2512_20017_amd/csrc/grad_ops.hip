@@ -172,14 +172,14 @@ struct GradEnd {
 // One workgroup of kThreads: adds the slots of each tensor of the table, and the tensors to the total of the tables before it;
 // returns the factor. All slots are on their way before the first is waited for (one by one they took 8 us instead of 5).
 // The order of the additions depends on the table alone. kAgent: the slots were stored by the running launch.
-template <int kThreads, int kSlots, bool kAgent>
-__device__ __forceinline__ float finish(const GradTable& tab, const GradEnd& end, bool write)
+template <int kThreads, int kSlots, bool kAgent, class Table>
+__device__ __forceinline__ float finish(const Table& tab, const GradEnd& end, bool write)
 {
     __shared__ double sSlot[kSlots];
-    __shared__ double sTensor[kGradTableTensors];
-    __shared__ uint32_t sFirst[kGradTableTensors + 1];
+    __shared__ double sTensor[Table::kTensors];
+    __shared__ uint32_t sFirst[Table::kTensors + 1];
     __shared__ float sScale;
-    static_assert(kThreads > kGradTableTensors, "");
+    static_assert(kThreads > Table::kTensors, "");
     constexpr int kEach = (kSlots + kThreads - 1) / kThreads;
     const uint32_t count = tab.count, blocks = tab.blocks, lane = threadIdx.x & 63;
     double mine[kEach];
@@ -234,7 +234,8 @@ __device__ __forceinline__ float finish(const GradTable& tab, const GradEnd& end
     return sScale;
 }
 
-__global__ __launch_bounds__(1024) void k_grad_finish(GradEnd end, GradTable tab)
+template <class Table>
+__global__ __launch_bounds__(1024) void k_grad_finish(GradEnd end, Table tab)
 {
     finish<1024, kGradSlots, false>(tab, end, true);
 }
@@ -244,8 +245,8 @@ __global__ __launch_bounds__(1024) void k_grad_finish(GradEnd end, GradTable tab
 // Masks that come several units early, units of more planes and 4,096 workgroups made the latter 3 to 40 % slower.
 // kAlone: the last workgroup to be done finishes in the same launch: slots go past the caches of the eight dies (agent scope), and
 // the counter is left at zero for the next launch.
-template <bool kAlone>
-__global__ __launch_bounds__(kGradBlock, 8) void k_grad_squares(GradEnd end, GradTable tab)
+template <bool kAlone, class Table>
+__global__ __launch_bounds__(kGradBlock, 8) void k_grad_squares(GradEnd end, Table tab)
 {
     __shared__ double sWave[kGradBlock / 64];
     __shared__ bool sLast;
@@ -373,8 +374,8 @@ __device__ void write_scaled(const GradTensorDev& t, float scale, uint32_t first
 // written, 7.2 TB/s: most of what is read is still in the last-level cache, since nothing else of the two passes goes there. 2M
 // surfels, twice what it holds: 148 us, 6.5 TB/s. kFinish: every workgroup adds the slots up for itself, one writes the result: for
 // small lists, whose sums then need no ending.
-template <bool kFinish>
-__global__ __launch_bounds__(kGradBlock, 8) void k_grad_scale(GradEnd end, GradTable tab)
+template <bool kFinish, class Table>
+__global__ __launch_bounds__(kGradBlock, 8) void k_grad_scale(GradEnd end, Table tab)
 {
     const uint32_t block = gridDim.x - 1 - blockIdx.x;      // backwards: the end of the gradient was read last
     const uint32_t ti = find_tensor(tab, block);
@@ -493,7 +494,8 @@ __device__ __forceinline__ void adam_tensor(const AdamTensorDev& t, const AdamDe
     }
 }
 
-__global__ __launch_bounds__(kGradBlock) void k_adam_list(AdamTable tab, const float* __restrict__ result)
+template <class Table>
+__global__ __launch_bounds__(kGradBlock) void k_adam_list(Table tab, const float* __restrict__ result)
 {
     const uint32_t block = gridDim.x - 1 - blockIdx.x;      // backwards: the norm has read the end of the gradient last
     const uint32_t ti = find_tensor(tab, block);
@@ -536,11 +538,12 @@ static uint32_t cut_blocks(Table& tab, uint64_t units, uint32_t most)
     return at;
 }
 
-// Up to kGradTableTensors of a list; tensors without entries keep their place and get no unit.
-static uint64_t fill_table(GradTable& tab, const GradTensorDev* list, int count)
+// As many tensors of a list as the table holds; tensors without entries keep their place and get no unit.
+template <class Table>
+static uint64_t fill_table(Table& tab, const GradTensorDev* list, uint32_t count)
 {
     uint64_t units = 0;
-    tab.count = (uint32_t)(count < kGradTableTensors ? count : kGradTableTensors);
+    tab.count = count < Table::kTensors ? count : Table::kTensors;
     for (uint32_t i = 0; i < tab.count; ++i) {
         tab.t[i] = list[i];
         units += tab.t[i].units = units_of(list[i]);
@@ -548,62 +551,74 @@ static uint64_t fill_table(GradTable& tab, const GradTensorDev* list, int count)
     return units;
 }
 
-template <class Args>
-constexpr bool fits_kernel_arguments() { return sizeof(Args) + sizeof(GradEnd) <= 4096; }
-static_assert(fits_kernel_arguments<GradTable>() && fits_kernel_arguments<AdamTable>(), "");
+static_assert(sizeof(GradTable<kGradTableTensors>) + sizeof(GradEnd) <= 4096 && sizeof(AdamTable<kAdamTableTensors>) + sizeof(void*) <= 4096, "");
 
-hipError_t launch_grad(int count, const GradTensorDev* list, float max_norm, float* result, GradWorkspace* ws, bool clip, hipStream_t s)
+template <class Table>
+static void grad_launches(uint32_t count, const GradTensorDev* list, float max_norm, float* result, GradWorkspace* ws, bool clip, hipStream_t s)
 {
-    GradTable tab;
+    Table tab;
     bool scaled = !clip;
     {
         ProfScope prof(kKGradNorm, s);
-        int at = 0;
+        uint32_t at = 0;
         do {
             const uint64_t units = fill_table(tab, list + at, count - at);
             const uint32_t blocks = cut_blocks(tab, units, kGradBlocks);
-            const GradEnd end{ws, result, result + 2 + at, max_norm, at == 0, at + (int)tab.count == count};
+            const GradEnd end{ws, result, result + 2 + at, max_norm, at == 0, at + tab.count == count};
             const dim3 grid(blocks ? blocks : 1), block(kGradBlock);
             if (blocks && blocks <= kInlineSlots && units <= kGradBlocks && clip && end.first_table && end.last_table) {      // a workgroup per unit
-                hipLaunchKernelGGL(k_grad_squares<false>, grid, block, 0, s, end, tab);
-                hipLaunchKernelGGL(k_grad_scale<true>, grid, block, 0, s, end, tab);
+                hipLaunchKernelGGL((k_grad_squares<false, Table>), grid, block, 0, s, end, tab);
+                hipLaunchKernelGGL((k_grad_scale<true, Table>), grid, block, 0, s, end, tab);
                 scaled = true;
             } else if (blocks <= kAloneSlots) {
-                hipLaunchKernelGGL(k_grad_squares<true>, grid, block, 0, s, end, tab);
+                hipLaunchKernelGGL((k_grad_squares<true, Table>), grid, block, 0, s, end, tab);
             } else {
-                hipLaunchKernelGGL(k_grad_squares<false>, grid, block, 0, s, end, tab);
-                hipLaunchKernelGGL(k_grad_finish, dim3(1), dim3(1024), 0, s, end, tab);
+                hipLaunchKernelGGL((k_grad_squares<false, Table>), grid, block, 0, s, end, tab);
+                hipLaunchKernelGGL(k_grad_finish<Table>, dim3(1), dim3(1024), 0, s, end, tab);
             }
-            at += (int)tab.count;
+            at += tab.count;
         } while (at < count);
     }
     if (!scaled) {
         ProfScope prof(kKGradScale, s);
-        for (int at = 0; at < count; at += (int)tab.count) {
+        for (uint32_t at = 0; at < count; at += tab.count) {
             const uint64_t units = fill_table(tab, list + at, count - at);
             const uint32_t blocks = cut_blocks(tab, units, kMostBlocks);
             const GradEnd end{ws, result, result + 2 + at, max_norm, 0, 0};
-            if (blocks) hipLaunchKernelGGL(k_grad_scale<false>, dim3(blocks), dim3(kGradBlock), 0, s, end, tab);
+            if (blocks) hipLaunchKernelGGL((k_grad_scale<false, Table>), dim3(blocks), dim3(kGradBlock), 0, s, end, tab);
         }
     }
+}
+
+hipError_t launch_grad(int count, const GradTensorDev* list, float max_norm, float* result, GradWorkspace* ws, bool clip, hipStream_t s)
+{
+    if ((uint32_t)count <= kShortTable) grad_launches<GradTable<kShortTable>>(count, list, max_norm, result, ws, clip, s);
+    else grad_launches<GradTable<kGradTableTensors>>(count, list, max_norm, result, ws, clip, s);
     return hipGetLastError();
 }
 
-hipError_t launch_adam_list(int count, const AdamTensorDev* list, const AdamDev& adam, const float* result, hipStream_t s)
+template <class Table>
+static void adam_launches(uint32_t count, const AdamTensorDev* list, const AdamDev& adam, const float* result, hipStream_t s)
 {
-    ProfScope prof(kKAdamList, s);
-    AdamTable tab;
+    Table tab;
     tab.adam = adam;
-    for (int at = 0; at < count; at += (int)tab.count) {
+    for (uint32_t at = 0; at < count; at += tab.count) {
         uint64_t units = 0;
-        tab.count = (uint32_t)(count - at < kAdamTableTensors ? count - at : kAdamTableTensors);
+        tab.count = count - at < Table::kTensors ? count - at : Table::kTensors;
         for (uint32_t i = 0; i < tab.count; ++i) {
             tab.t[i] = list[at + i];
             units += tab.t[i].units = units_of(tab.t[i]);
         }
         const uint32_t blocks = cut_blocks(tab, units, kMostBlocks);
-        if (blocks) hipLaunchKernelGGL(k_adam_list, dim3(blocks), dim3(kGradBlock), 0, s, tab, result);
+        if (blocks) hipLaunchKernelGGL(k_adam_list<Table>, dim3(blocks), dim3(kGradBlock), 0, s, tab, result);
     }
+}
+
+hipError_t launch_adam_list(int count, const AdamTensorDev* list, const AdamDev& adam, const float* result, hipStream_t s)
+{
+    ProfScope prof(kKAdamList, s);
+    if ((uint32_t)count <= kShortTable) adam_launches<AdamTable<kShortTable>>(count, list, adam, result, s);
+    else adam_launches<AdamTable<kAdamTableTensors>>(count, list, adam, result, s);
     return hipGetLastError();
 }
 
