@@ -406,6 +406,29 @@ def test_two_graphs_share_a_workspace_and_streams_change():
                 assert all(torch.equal(a, b) for a, b in zip(flat(s), flat(ref))), (k, rep)
 
 
+def test_calls_in_flight_on_two_streams():
+    """Lists of both kinds of ending, each stream with a workspace and result of its own, nothing waiting between."""
+    pairs = []
+    for spec in (SPECS["odd rows"], SPECS["more than a workgroup each"]):
+        ts, ms = make(spec, len(spec))
+        pairs.append((B.GradList(ts, visible=ms), B.GradList(ts, visible=ms, out=[torch.zeros_like(t) for t in ts]), len(ts)))
+    want = []
+    for norm, _, count in pairs:
+        result = torch.empty(2 + count, device="cuda")
+        B.pbdr_grad_norm(norm, 0.5, result, B.alloc_grad_workspace(count))
+        want.append(result)
+    streams = [torch.cuda.Stream() for _ in pairs]
+    spaces = [B.alloc_grad_workspace(count) for *_, count in pairs]
+    results = [[torch.empty(2 + count, device="cuda") for _ in range(20)] for *_, count in pairs]
+    torch.cuda.synchronize()
+    for rep in range(20):
+        for (norm, clip, _), stream, ws, result in zip(pairs, streams, spaces, results):
+            (B.pbdr_grad_clip if rep % 3 == 2 else B.pbdr_grad_norm)(clip if rep % 3 == 2 else norm, 0.5, result[rep], ws, stream=stream)
+    torch.cuda.synchronize()
+    for result, w in zip(results, want):
+        assert all(torch.equal(r, w) for r in result)
+
+
 def test_lists_follow_tensors_that_get_other_memory():
     t, mask = torch.ones(3, 50, device="cuda"), torch.ones(50, dtype=torch.bool, device="cuda")
     mask[10:] = False
