@@ -868,7 +868,7 @@ int pbdr_adam_selective_list(int32_t num_tensors, const pbdr_adam_tensor* tensor
         const pbdr_adam_tensor& t = tensors[i];
         if (!check_extent(t.n, t.planes) || !(t.lr >= 0.f)) return PBDR_ERR_INVALID_ARG;
         const AdamDev a = make_adam(t.lr, cfg->beta1, cfg->beta2, cfg->eps, cfg->step, cfg->zero_grad);      // of which the step size is the tensor's own
-        list[i] = AdamTensorDev{t.param, t.grad, t.exp_avg, t.exp_avg_sq, t.visible, (uint64_t)t.n, (uint32_t)t.planes, 0u, a.step_size};
+        list[i] = AdamTensorDev{t.param, t.grad, t.exp_avg, t.exp_avg_sq, t.visible, (uint64_t)t.n, (uint32_t)t.planes, 0u, 0u, a.step_size};
         const uint64_t bytes = list[i].n * list[i].planes * sizeof(float);
         if (bytes == 0) continue;
         if (!aligned16(t.param) || !aligned16(t.grad) || !aligned16(t.exp_avg) || !aligned16(t.exp_avg_sq) || (t.visible && !aligned16(t.visible)))

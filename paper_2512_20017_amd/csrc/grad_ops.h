@@ -7,15 +7,21 @@ namespace pbdr {
 enum { kGradF32 = 0, kGradF16 = 1, kGradBF16 = 2 };
 
 constexpr int kGradBlock = 256;
-constexpr int kDenseVecs = 2;                     // vectors of a lane in a unit of a tensor without mask (2, 4, 8: the same within 2 %)
-// Planes of a masked unit, all of which are read before the first is used. Sums and scaling: 4 (8M points, a quarter used: norm
-// 97 us, clipped into buffers of their own 386; 8 planes 98 and 425, 6 between). Adam reads four vectors a plane: 2 (8M points, a
-// quarter used, with the norm: 736 us; 1 plane 766, 3 planes 740, 4 750; 1M points 207 each; 200,003 surfels 56, 3 and 4 planes 57).
+// Vectors of a lane in a unit of a tensor without mask: 1M points' norm 42.4 us, clipped 109; 4 vectors 43.3 and 116.
+constexpr int kDenseVecs = 2;
+// Planes of a masked unit that sums or scales, all of which are read before the first is used (8M points, a quarter used: norm 97 us;
+// 2 planes 136, 3 planes 97, 8 planes 100, where scaling runs out of registers).
 constexpr uint32_t kMaskPlanes = 4;
-constexpr uint32_t kAdamPlanes = 2;
+// A workgroup that finds nothing to do still costs half a nanosecond of the launch, and large scenes are seen in small part: from
+// kManyPoints on a workgroup scales kScaleRun units (8M points clipped: 5 % used 174 -> 130 us, 25 % used 377 and 379) and Adam takes
+// eight planes a unit instead of two (5 % used 319 -> 223, 10 % 382 -> 339, 25 % 738 -> 748). Below, workgroups have to be many
+// enough to fill the chip evenly: four planes (1.5M points, 5 % used 69 -> 60 us; 8 planes 54, but 1M points, 60 % used, 212 instead of
+// 208), and one below kFewPoints (200,003 surfels, 70 % used: 54 us; 2 planes 56, 4 planes 58, 8 planes 61).
+constexpr uint64_t kFewPoints = 400000, kManyPoints = 4000000;
+constexpr uint32_t kScaleRun = 4;
 // Workgroups of a launch that sums, eight per compute unit: units that need no reading leave gaps in masked tensors (8M points, a
-// quarter used: norm 99 us; 1,024 workgroups 113, 512 168; 4,096 103). Tensors without mask take half as many for their units, and
-// stream better so (1M points: norm 43.7 us against 45.8).
+// quarter used: norm 97.5 us; 1,024 workgroups 113; 4,096 96.5, but 1M points without mask 45.9 instead of 42.4). Tensors without
+// mask take half as many for their units, and stream better so (1M points 43.7 us against 45.8).
 constexpr uint32_t kGradBlocks = 2048;
 constexpr uint32_t kLineFloats = 32;              // of a cache line
 constexpr uint32_t kMostBlocks = 1u << 23;        // of a launch: fewer than 2^32 threads
@@ -35,7 +41,7 @@ struct GradTensorDev {
 template <uint32_t kMost>
 struct GradTable {
     static constexpr uint32_t kTensors = kMost;
-    uint32_t count, blocks;
+    uint32_t count, blocks, each;                 // each: factor on the units that a workgroup takes in a row
     uint32_t first[kMost + 1];                    // first workgroup of each tensor, and their number
     GradTensorDev t[kMost];
 };
@@ -45,12 +51,13 @@ struct AdamTensorDev {
     const uint8_t* visible;
     uint64_t n;
     uint32_t planes, units;
+    uint32_t unit;             // planes of a unit of a masked tensor
     float step_size;
 };
 template <uint32_t kMost>
 struct AdamTable {
     static constexpr uint32_t kTensors = kMost;
-    uint32_t count, blocks;
+    uint32_t count, blocks, each;
     uint32_t first[kMost + 1];
     AdamDev adam;              // of every tensor but for step_size
     AdamTensorDev t[kMost];
@@ -58,11 +65,11 @@ struct AdamTable {
 
 // a slot per workgroup that sums: a table has kGradBlocks of them at most, and one more per tensor whose units do not come out even
 constexpr uint32_t kGradSlots = kGradBlocks + kGradTableTensors;
-// Workgroups up to which one launch sums and finishes: 32 to 128 workgroups 8.3 us a call, 11 with a launch of its own for the
-// end; 250 workgroups 10.5 and 10.3; 500 15.3 and 10.5.
-constexpr uint32_t kAloneSlots = 128;
-// Workgroups up to which every workgroup that scales adds the slots up itself: 128 to 500 workgroups 11.9 us a call, 13.2 to 15.7
-// with a launch between; 1,000 workgroups 12.1 and 15.7; 2,000 16.3 and 15.9.
+// Workgroups up to which one launch sums and finishes: up to 64 workgroups 6.1 us a call, 130 6.7, 250 8.8, 500 13.4; with a launch of
+// its own for the end 9.2 to 9.5.
+constexpr uint32_t kAloneSlots = 256;
+// Workgroups up to which every workgroup that scales adds the slots up itself: 130 to 500 workgroups 9.7 us a call, 1,000 10.1, 2,000
+// 13.6; with a launch between 13.0 to 14.0.
 constexpr uint32_t kInlineSlots = 1024;
 struct GradWorkspace {
     uint32_t done;             // workgroups of the running launch that have stored their sum; zero between launches

@@ -294,8 +294,11 @@ __device__ __forceinline__ void store_vec(Vec v, T* to)
     __builtin_nontemporal_store(v, reinterpret_cast<Vec*>(to));
 }
 
+// units that a workgroup which scales takes in a row
+__host__ __device__ __forceinline__ uint32_t scale_run(const GradTensorDev& t) { return t.visible && t.n >= kManyPoints ? kScaleRun : 1; }
+
 template <int kDtype>
-__device__ void write_scaled(const GradTensorDev& t, float scale, uint32_t first, uint32_t step)
+__device__ void write_scaled(const GradTensorDev& t, float scale, uint32_t begin, uint32_t end)
 {
     using T = typename GradType<kDtype>::T;
     using Vec = typename GradVec<T>::V;
@@ -306,7 +309,7 @@ __device__ void write_scaled(const GradTensorDev& t, float scale, uint32_t first
     const uint64_t count = t.n * t.planes;
     if (t.visible == nullptr) {
         constexpr uint32_t kUnit = kGradBlock * kN * kDenseVecs;
-        for (uint32_t u = first; u < t.units; u += step) {
+        for (uint32_t u = begin; u < end; ++u) {
             const uint64_t base = (uint64_t)u * kUnit + threadIdx.x * kN;
             Vec v[kDenseVecs];
             if ((uint64_t)(u + 1) * kUnit <= count) {
@@ -329,7 +332,7 @@ __device__ void write_scaled(const GradTensorDev& t, float scale, uint32_t first
             }
         }
     } else {
-        for (uint32_t u = first; u < t.units; u += step) {
+        for (uint32_t u = begin; u < end; ++u) {
             const MaskedUnit w = masked_unit<kN>(u, t.planes);
             const typename MaskOf<kN>::T mask = mask_bytes<kN>(t.visible, w.at, t.n);
             if (mask == 0) continue;
@@ -370,7 +373,7 @@ __device__ void write_scaled(const GradTensorDev& t, float scale, uint32_t first
     }
 }
 
-// One unit per workgroup (2,048 workgroups that walk over the units took 4 to 10 % longer). 1M points SH3: 66 us for 236 MB read and
+// One unit per workgroup (2,048 workgroups that walk over the units took 4 to 10 % longer), four of a masked tensor of many points. 1M points SH3: 66 us for 236 MB read and
 // written, 7.2 TB/s: most of what is read is still in the last-level cache, since nothing else of the two passes goes there. 2M
 // surfels, twice what it holds: 148 us, 6.5 TB/s. kFinish: every workgroup adds the slots up for itself, one writes the result: for
 // small lists, whose sums then need no ending.
@@ -382,14 +385,14 @@ __global__ __launch_bounds__(kGradBlock, 8) void k_grad_scale(GradEnd end, Table
     const GradTensorDev& t = tab.t[ti];
     const float scale = kFinish ? finish<kGradBlock, kInlineSlots, false>(tab, end, blockIdx.x == 0) : end.result[1];
     if (scale == 1.f && t.out == t.data) return;      // nothing would change
-    const uint32_t first = block - tab.first[ti], step = tab.first[ti + 1] - tab.first[ti];
-    if (t.dtype == kGradF32) write_scaled<kGradF32>(t, scale, first, step);
-    else if (t.dtype == kGradF16) write_scaled<kGradF16>(t, scale, first, step);
-    else write_scaled<kGradBF16>(t, scale, first, step);
+    const uint32_t run = tab.each * scale_run(t), begin = (block - tab.first[ti]) * run, stop = min(begin + run, t.units);
+    if (t.dtype == kGradF32) write_scaled<kGradF32>(t, scale, begin, stop);
+    else if (t.dtype == kGradF16) write_scaled<kGradF16>(t, scale, begin, stop);
+    else write_scaled<kGradBF16>(t, scale, begin, stop);
 }
 
 // Adam, a unit per workgroup: 28 bytes an entry, and the gradient's four again. 1M points SH3, 60 % used: 173 us for 0.96 GB beside a
-// gradient that is still cached, 5.5 TB/s; 8M points, a quarter used: 639 us for 3.2 GB and 0.46 GB of gradient, 5.7 TB/s. With
+// gradient that is still cached, 5.5 TB/s; 8M points, a quarter used: 648 us for 3.2 GB and 0.46 GB of gradient, 5.7 TB/s. With
 // ordinary loads and stores of parameters and moments 203 us at 1M points, forwards 680 us at 8M.
 // A lane takes four entries of a row, and a workgroup's stretch of a row begins on a cache line of the moments, wherever the row
 // begins: lines that two wavefronts write in part cost 12 % of the whole (with the norm 200,003 surfels 64 us, 200,000 surfels 57). So
@@ -462,35 +465,29 @@ __device__ __forceinline__ void adam_store(const AdamDev& c, uint32_t mask, cons
     }
 }
 
-// without a mask the tensor is one row
+// Without a mask the tensor is one row. With one a unit is t.unit planes of a stretch, taken one at a time.
 template <bool kMasked>
-__device__ __forceinline__ void adam_tensor(const AdamTensorDev& t, const AdamDev& c, float scale, uint32_t first, uint32_t step)
+__device__ __forceinline__ void adam_tensor(const AdamTensorDev& t, const AdamDev& c, float scale, uint32_t begin, uint32_t end)
 {
-    constexpr uint32_t kPlanes = kMasked ? kAdamPlanes : 1;
-    const uint32_t rows = kMasked ? t.planes : 1, groups = (rows + kPlanes - 1) / kPlanes;
+    const uint32_t rows = kMasked ? t.planes : 1, unit = kMasked ? t.unit : 1, groups = (rows + unit - 1) / unit;
     const int64_t n = (int64_t)(kMasked ? t.n : t.n * t.planes);
-    for (uint32_t u = first; u < t.units; u += step) {
-        const uint32_t seg = u / groups, p0 = (u - seg * groups) * kPlanes;
-        int64_t at[kPlanes];
-        uint32_t mask[kPlanes], any = 0;
-#pragma unroll
-        for (uint32_t j = 0; j < kPlanes; ++j) {
-            const uint64_t row = (uint64_t)(p0 + j) * n;
-            at[j] = ((int64_t)seg * kGradBlock + threadIdx.x) * 4 - (int64_t)((reinterpret_cast<uintptr_t>(t.m + row) >> 2) & (kLineFloats - 1));
-            mask[j] = p0 + j < rows ? adam_mask<kMasked>(t.visible, at[j], n) : 0u;
-            any |= mask[j];
+    for (uint32_t u = begin; u < end; ++u) {
+        const uint32_t seg = u / groups, p0 = (u - seg * groups) * unit, p1 = min(p0 + unit, rows);
+        const int64_t at0 = ((int64_t)seg * kGradBlock + threadIdx.x) * 4;
+        if (kMasked && unit > 1) {      // leave at once if no lane will have a used point, wherever the planes begin on a line
+            const uint32_t before = threadIdx.x < kLineFloats / 4 ? adam_mask<true>(t.visible, at0 - (int64_t)kLineFloats, n) : 0u;
+            if (!__syncthreads_or((int)(adam_mask<true>(t.visible, at0, n) | before))) continue;
         }
-        if (any == 0) continue;
-        AdamVec x[kPlanes];
-#pragma unroll
-        for (uint32_t j = 0; j < kPlanes; ++j)
-            if (mask[j]) x[j] = adam_load(t, (uint64_t)(p0 + j) * n, at[j], n);
-#pragma unroll
-        for (uint32_t j = 0; j < kPlanes; ++j)
-            if (mask[j]) {
-                adam_step(c, scale, mask[j], x[j]);
-                adam_store(c, mask[j], t, (uint64_t)(p0 + j) * n, at[j], n, x[j]);
-            }
+#pragma unroll 1
+        for (uint32_t p = p0; p < p1; ++p) {
+            const uint64_t row = (uint64_t)p * n;
+            const int64_t at = at0 - (int64_t)((reinterpret_cast<uintptr_t>(t.m + row) >> 2) & (kLineFloats - 1));
+            const uint32_t mask = adam_mask<kMasked>(t.visible, at, n);
+            if (mask == 0) continue;
+            AdamVec x = adam_load(t, row, at, n);
+            adam_step(c, scale, mask, x);
+            adam_store(c, mask, t, row, at, n, x);
+        }
     }
 }
 
@@ -503,9 +500,9 @@ __global__ __launch_bounds__(kGradBlock) void k_adam_list(Table tab, const float
     const float scale = result ? result[1] : 1.f;
     AdamDev c = tab.adam;
     c.step_size = t.step_size;
-    const uint32_t first = block - tab.first[ti], step = tab.first[ti + 1] - tab.first[ti];
-    if (t.visible) adam_tensor<true>(t, c, scale, first, step);
-    else adam_tensor<false>(t, c, scale, first, step);
+    const uint32_t begin = (block - tab.first[ti]) * tab.each, end = min(begin + tab.each, t.units);
+    if (t.visible) adam_tensor<true>(t, c, scale, begin, end);
+    else adam_tensor<false>(t, c, scale, begin, end);
 }
 
 static uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
@@ -517,25 +514,39 @@ static uint32_t units_of(const GradTensorDev& t)
     if (t.visible == nullptr) return (uint32_t)ceil_div(t.n * t.planes, kGradBlock * vec * kDenseVecs);
     return (uint32_t)(ceil_div(t.n, kGradBlock * vec) * ceil_div(t.planes, kMaskPlanes));
 }
+static uint32_t adam_unit(const AdamTensorDev& t) { return t.n < kFewPoints ? 1 : t.n < kManyPoints ? 4 : 8; }
 static uint32_t units_of(const AdamTensorDev& t)      // lanes may stand before the begin of a row by a line less one
 {
     if (t.n == 0 || t.planes == 0) return 0;
     if (t.visible == nullptr) return (uint32_t)ceil_div(t.n * t.planes + kLineFloats - 1, kGradBlock * 4);
-    return (uint32_t)(ceil_div(t.n + kLineFloats - 1, kGradBlock * 4) * ceil_div(t.planes, kAdamPlanes));
+    return (uint32_t)(ceil_div(t.n + kLineFloats - 1, kGradBlock * 4) * ceil_div(t.planes, t.unit));
 }
 
-// The workgroups of a table: one per unit, or, with more than `most` units, equal runs of them.
+// The workgroups that sum a table: one per unit, or, with more than kGradBlocks units, that many and each as many units.
 template <class Table>
-static uint32_t cut_blocks(Table& tab, uint64_t units, uint32_t most)
+static uint32_t cut_sums(Table& tab, uint64_t units)
 {
-    const uint64_t each = units > most ? ceil_div(units, most) : 1;
+    const uint64_t each = units > kGradBlocks ? ceil_div(units, kGradBlocks) : 1;
     uint32_t at = 0;
     for (uint32_t i = 0; i < tab.count; ++i) {
         tab.first[i] = at;
         at += (uint32_t)ceil_div(tab.t[i].units, tab.t[i].visible || each == 1 ? each : 2 * each);
     }
-    tab.blocks = tab.first[tab.count] = at;
-    return at;
+    tab.each = 1;
+    return tab.blocks = tab.first[tab.count] = at;
+}
+
+// The workgroups that scale or update a table: one per run of units, and longer runs only where a launch could not have as many.
+template <class Table, class Run>
+static uint32_t cut_runs(Table& tab, uint64_t units, Run run)
+{
+    tab.each = (uint32_t)ceil_div(units + 1, kMostBlocks);
+    uint32_t at = 0;
+    for (uint32_t i = 0; i < tab.count; ++i) {
+        tab.first[i] = at;
+        at += (uint32_t)ceil_div(tab.t[i].units, (uint64_t)tab.each * run(tab.t[i]));
+    }
+    return tab.blocks = tab.first[tab.count] = at;
 }
 
 // As many tensors of a list as the table holds; tensors without entries keep their place and get no unit.
@@ -563,7 +574,7 @@ static void grad_launches(uint32_t count, const GradTensorDev* list, float max_n
         uint32_t at = 0;
         do {
             const uint64_t units = fill_table(tab, list + at, count - at);
-            const uint32_t blocks = cut_blocks(tab, units, kGradBlocks);
+            const uint32_t blocks = cut_sums(tab, units);
             const GradEnd end{ws, result, result + 2 + at, max_norm, at == 0, at + tab.count == count};
             const dim3 grid(blocks ? blocks : 1), block(kGradBlock);
             if (blocks && blocks <= kInlineSlots && units <= kGradBlocks && clip && end.first_table && end.last_table) {      // a workgroup per unit
@@ -583,7 +594,7 @@ static void grad_launches(uint32_t count, const GradTensorDev* list, float max_n
         ProfScope prof(kKGradScale, s);
         for (uint32_t at = 0; at < count; at += tab.count) {
             const uint64_t units = fill_table(tab, list + at, count - at);
-            const uint32_t blocks = cut_blocks(tab, units, kMostBlocks);
+            const uint32_t blocks = cut_runs(tab, units, scale_run);
             const GradEnd end{ws, result, result + 2 + at, max_norm, 0, 0};
             if (blocks) hipLaunchKernelGGL((k_grad_scale<false, Table>), dim3(blocks), dim3(kGradBlock), 0, s, end, tab);
         }
@@ -607,9 +618,10 @@ static void adam_launches(uint32_t count, const AdamTensorDev* list, const AdamD
         tab.count = count - at < Table::kTensors ? count - at : Table::kTensors;
         for (uint32_t i = 0; i < tab.count; ++i) {
             tab.t[i] = list[at + i];
+            tab.t[i].unit = adam_unit(tab.t[i]);
             units += tab.t[i].units = units_of(tab.t[i]);
         }
-        const uint32_t blocks = cut_blocks(tab, units, kMostBlocks);
+        const uint32_t blocks = cut_runs(tab, units, [](const AdamTensorDev&) { return 1u; });
         if (blocks) hipLaunchKernelGGL(k_adam_list<Table>, dim3(blocks), dim3(kGradBlock), 0, s, tab, result);
     }
 }

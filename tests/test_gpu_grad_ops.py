@@ -110,6 +110,7 @@ SPECS = {
     "nothing used": [((3, 777), F32, 0.0), ((2, 100), F16, 0.0)],
     "one of many used": [((3, 1500), F32, 0.0), ((3, 1500), F32, 0.001), ((1,), F32, None)],
     "empty tensors": [((0,), F32, None), ((3, 0), F32, None), ((10,), F32, None), ((0, 4), F16, None), ((3, 0), BF16, 0.5)],
+    "many points": [((11, 4_000_005), F32, 0.0003), ((9, 4_000_001), BF16, 0.4), ((3, 4_000_000), F32, 0.3)],
     "more than a workgroup each": [((3, 1_000_001), F32, 0.4), ((9_000_001,), F32, None), ((2, 3_000_000), BF16, 0.4)],
 }
 
@@ -229,6 +230,7 @@ ADAM_SPECS = {
     "eight": [((9,), F32, None)] * 8,
     "nine": [((3, 501), F32, 0.5)] * 9,
     "forty-nine": [((2, 77), F32, 0.5)] * 49,
+    "many points": [((11, 4_000_005), F32, 0.0003), ((4_000_005,), F32, 0.5), ((6, 400_000), F32, 0.0005), ((5, 399_999), F32, 0.2)],
     "large": [((48, 100_001), F32, 0.4), ((5_000_003,), F32, None)],
 }
 
@@ -318,7 +320,7 @@ def test_refusals_on_the_gpu():
     assert (t == 1).all()
 
 
-@pytest.mark.parametrize("n", [1, 3, 31, 33, 1023, 1025, 2050, 40_003])
+@pytest.mark.parametrize("n", [1, 3, 31, 33, 1023, 1025, 2050, 40_003, 450_001, 4_100_001])
 @pytest.mark.parametrize("masked", [True, False])
 def test_rows_and_buffers_that_begin_anywhere_on_a_line(n, masked):
     """Parameter, gradient, moments and output each at another multiple of 16 bytes, rows at any multiple of a value: what lies
