@@ -439,7 +439,8 @@ int pbdr_preprocess_bwd_batch_adam(const pbdr_scene* scene, int32_t num_views, c
  *
  * pbdr_adam_selective_list = pbdr_adam_selective on every tensor of the list with the gradient result[1] * grad (rounded
  * to 32 bits; 0 where result[1] is 0: moments decay and parameters follow them, nothing of a broken batch gets in), bit for
- * bit what pbdr_grad_clip and those calls leave, without the clipped gradient going through memory. result: what pbdr_grad_norm wrote, or NULL: no clipping. visible == NULL: every point.
+ * bit what pbdr_grad_clip and those calls leave, without the clipped gradient going through memory. result: what
+ * pbdr_grad_norm wrote, or NULL: no clipping. visible == NULL: every point.
  * cfg->lr is not used, each tensor has its own. cfg->zero_grad clears the used entries of grad.
  *
  * What a call writes must not overlap anything else that it reads or writes (a tensor twice in a list that is clipped or
