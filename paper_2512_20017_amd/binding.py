@@ -427,10 +427,15 @@ def pbdr_adam_selective(param, grad, exp_avg, exp_avg_sq, visible, lr, beta1, be
 _GRAD_DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
+# All that the description of a tensor rests on. Each look is one map() over the list: 167 tensors take 37 us of the host's time (the
+# address alone 7), the 5 of a scene 1.7; the time goes by tensors and looks, one by one in a loop it is the same.
+_LOOKS = (torch.Tensor.data_ptr, torch.Tensor.shape.__get__, torch.Tensor.dtype.__get__, torch.Tensor.is_contiguous, torch.Tensor.get_device)
+
+
 class _TensorList:
-    """Tensors of one device as an array of C structs. Before each call the list looks whether a tensor has got other memory since
-    (`t.data = ...`), and then describes them again. It holds the tensors and the memory that it has described, so that no other
-    memory comes to lie at the same address."""
+    """Tensors of one device as an array of C structs. Before each call the list looks whether a tensor or mask has got another
+    address, shape, type, device or order since (`t.data = ...`, `t.resize_(...)`), and then describes and checks them again. It
+    holds the tensors and the memory that it has described."""
 
     def __init__(self, columns, visible):
         count = len(columns[0])
@@ -442,13 +447,17 @@ class _TensorList:
             raise ValueError("pbdr: one mask for all tensors, or one (or None) for each")
         self._columns = [list(c) for c in columns]
         self._visible = list(visible)
-        self._all = [t for c in (*self._columns, self._visible) for t in c if t is not None]
+        self._all = list({id(t): t for c in (*self._columns, self._visible) for t in c if t is not None}.values())
         self._describe()
 
     def __len__(self):
         return len(self._columns[0])
 
+    def _look(self):
+        return [list(map(look, self._all)) for look in _LOOKS]
+
     def _describe(self):
+        seen = self._look()
         self.device = self._all[0].device if self._all else None
         for t in self._all:
             if t.device != self.device:
@@ -470,10 +479,10 @@ class _TensorList:
             sizes.append((n, t.numel() // n if n else 0))
         self._array = self._structs(sizes)
         self._memory = [t.untyped_storage() for t in self._all]
-        self._at = [t.data_ptr() for t in self._all]
+        self._seen = seen
 
     def array(self):
-        if list(map(torch.Tensor.data_ptr, self._all)) != self._at:
+        if self._look() != self._seen:
             self._describe()
         return self._array
 

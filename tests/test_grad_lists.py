@@ -143,3 +143,99 @@ def test_lists_of_the_binding_describe_and_refuse():
     assert adam_list.array()[0].lr == 0.5
     with pytest.raises(ValueError):
         adam_list.set_lrs([0.5, 0.5])
+
+
+# ------------------------------------------------------- tensors that change where they lie: what a list says of them changes with them
+def same_place(change, shape=(4, 6), dtype=torch.float32, mask=None):
+    """A list over a tensor at the begin of a larger buffer, described, then `change`; the address stays."""
+    t = torch.zeros(1000, dtype=dtype)[:24].view(shape)
+    at = t.data_ptr()
+    lists = [B.GradList([t], visible=mask), B.GradList([torch.zeros_like(t)], visible=mask, out=[t])]
+    if dtype == torch.float32:
+        lists.append(B.AdamList([torch.zeros_like(t)], [torch.zeros_like(t)], [t], [torch.zeros_like(t)], [1.0], visible=mask))
+    for a in lists:
+        a.array()
+    change(t)
+    assert t.data_ptr() == at
+    return t, lists
+
+
+def whole(t, shape):      # the buffer that t lies in, from its begin
+    return torch.empty(0, dtype=t.dtype).set_(t.untyped_storage(), 0, shape)
+
+
+@pytest.mark.parametrize("shape", [(4, 3), (2, 6), (4, 60), (9, 6), (24,), (1,)])
+@pytest.mark.parametrize("how", ["data", "resize_"])
+def test_a_tensor_that_grows_or_shrinks_in_place(shape, how):
+    def change(t):
+        if how == "data":
+            t.data = whole(t, shape)
+        else:
+            t.resize_(shape)
+    t = whole(torch.zeros(1000), (4, 6))
+    a = B.GradList([t])
+    change(t)
+    assert (a.array()[0].n, a.array()[0].planes) == (t.numel(), 1)
+    t = whole(torch.zeros(1000), (4, 6))
+    m, v, g = (whole(torch.zeros(1000), (4, 6)) for _ in range(3))
+    a = B.AdamList([t], [g], [m], [v], [1.0])
+    change(t)
+    with pytest.raises(ValueError):      # the others have not changed yet
+        a.array()
+    for x in (g, m, v):
+        change(x)
+    assert (a.array()[0].n, a.array()[0].planes) == (t.numel(), 1)
+
+
+@pytest.mark.parametrize("n", [3, 5, 7, 40])
+def test_a_mask_and_its_tensors_that_change_together(n):
+    t, mask = whole(torch.zeros(1000), (4, 6)), whole(torch.ones(100, dtype=torch.uint8), (6,))
+    a = B.GradList([t], visible=mask)
+    t.resize_(4, n)
+    with pytest.raises(ValueError):
+        a.array()
+    mask.resize_(n)
+    assert (a.array()[0].n, a.array()[0].planes) == (n, 4)
+    mask.resize_(n - 1)
+    with pytest.raises(ValueError):
+        a.array()
+
+
+def test_changes_in_place_that_no_list_takes():
+    mask = torch.ones(6, dtype=torch.uint8)
+    def transposed(t): t.data = whole(t, (6, 6)).t()
+    def strided(t): t.data = whole(t, (4, 12))[:, ::2]
+    def doubled(t): t.data = t.data.view(torch.float64)
+    def folded(t): t.data = t.data.view(2, 12)      # points other than the mask's
+    for change, with_mask in ((transposed, False), (strided, False), (strided, True), (doubled, False), (folded, True)):
+        _, lists = same_place(change, mask=mask if with_mask else None)
+        for a in lists:
+            with pytest.raises(ValueError):
+                a.array()
+    square = whole(torch.zeros(100), (6, 6))      # nothing but the order of its values changes
+    a = B.GradList([square])
+    square.t_()
+    with pytest.raises(ValueError):
+        a.array()
+    bits = torch.ones(6, dtype=torch.uint8)
+    a = B.GradList([torch.zeros(2, 6)], visible=bits)
+    bits.data = bits.data.view(torch.int8)
+    with pytest.raises(ValueError):
+        a.array()
+
+
+def test_a_type_that_changes_in_place():
+    t = torch.zeros(24, dtype=torch.float16)
+    a = B.GradList([t])
+    t.data = t.data.view(torch.bfloat16)
+    assert (a.array()[0].dtype, a.array()[0].n) == (2, 24)
+    t.data = t.data.view(torch.float32)
+    assert (a.array()[0].dtype, a.array()[0].n) == (0, 12)
+
+
+def test_a_list_is_described_once_while_nothing_changes():
+    t = torch.zeros(3, 8)
+    a = B.GradList([t], visible=torch.ones(8, dtype=torch.bool))
+    first = a.array()
+    t.add_(1.0)
+    assert a.array() is first
