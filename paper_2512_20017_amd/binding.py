@@ -435,7 +435,8 @@ _LOOKS = (torch.Tensor.data_ptr, torch.Tensor.shape.__get__, torch.Tensor.dtype.
 class _TensorList:
     """Tensors of one device as an array of C structs. Before each call the list looks whether a tensor or mask has got another
     address, shape, type, device or order since (`t.data = ...`, `t.resize_(...)`), and then describes and checks them again. It
-    holds the tensors and the memory that it has described."""
+    holds the tensors, not the memory they had when they were described: other memory at the same address, of the same device and
+    in the same form, is described by the same struct."""
 
     def __init__(self, columns, visible):
         count = len(columns[0])
@@ -478,7 +479,6 @@ class _TensorList:
             n = t.shape[-1]
             sizes.append((n, t.numel() // n if n else 0))
         self._array = self._structs(sizes)
-        self._memory = [t.untyped_storage() for t in self._all]
         self._seen = seen
 
     def array(self):

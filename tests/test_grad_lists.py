@@ -1,7 +1,9 @@
 """What the calls on lists of gradients refuse, before anything reaches a GPU: the C entries with addresses that are never
 followed, and the binding's lists with tensors on the CPU."""
 import ctypes as C
+import weakref
 
+import numpy as np
 import pytest
 import torch
 
@@ -239,3 +241,14 @@ def test_a_list_is_described_once_while_nothing_changes():
     first = a.array()
     t.add_(1.0)
     assert a.array() is first
+
+
+def test_a_list_does_not_keep_memory_that_its_tensors_have_left():
+    array = np.zeros((3, 8), dtype=np.float32)
+    left = weakref.ref(array)
+    t = torch.from_numpy(array)
+    lists = [B.GradList([t]), B.GradList([torch.zeros(3, 8)], out=[t]), B.AdamList([t], *[[torch.zeros(3, 8)] for _ in range(3)], [1.0])]
+    del array
+    assert left() is not None
+    t.data = torch.zeros(3, 8)
+    assert left() is None and len(lists) == 3
