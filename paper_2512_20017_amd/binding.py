@@ -459,10 +459,10 @@ class _TensorList:
 
     def _describe(self):
         seen = self._look()
-        self.device = self._all[0].device if self._all else None
+        device = self._all[0].device if self._all else None
         for t in self._all:
-            if t.device != self.device:
-                raise ValueError(f"pbdr: tensors of one list lie on {self.device} and {t.device}")
+            if t.device != device:
+                raise ValueError(f"pbdr: tensors of one list lie on {device} and {t.device}")
             if not t.is_contiguous():
                 raise ValueError(f"pbdr: a tensor of shape {tuple(t.shape)} and strides {t.stride()} is not contiguous")
         sizes = []
@@ -478,8 +478,8 @@ class _TensorList:
                 raise ValueError(f"pbdr: a mask of {tuple(v.shape)} {v.dtype} for a tensor of {tuple(t.shape)}: uint8 or bool, one per point")
             n = t.shape[-1]
             sizes.append((n, t.numel() // n if n else 0))
-        self._array = self._structs(sizes)
-        self._seen = seen
+        # together: a list that was refused is as it was, for tensors that go back to what they were
+        self.device, self._array, self._seen = device, self._structs(sizes), seen
 
     def array(self):
         if self._look() != self._seen:

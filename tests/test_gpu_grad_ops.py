@@ -511,3 +511,17 @@ def test_a_training_iteration_eager_and_replayed():
     r = ref["result"].double()
     assert float(r[0]) == pytest.approx(float(r[2:].norm()), rel=1e-6)
     assert float(r[7]) == pytest.approx(float(net.double().norm()), rel=1e-7)
+
+
+def test_a_list_that_was_refused_serves_tensors_that_came_back():
+    ts = [torch.full((40,), 3.0, device="cuda"), torch.full((30,), 4.0, device="cuda")]
+    gl = B.GradList(ts)
+    result, ws = torch.empty(4, device="cuda"), B.alloc_grad_workspace(2)
+    here = ts[0].data
+    ts[0].data = here.cpu()
+    with pytest.raises(ValueError):      # one on each side
+        B.pbdr_grad_norm(gl, 1.0, result, ws)
+    ts[0].data = here
+    B.pbdr_grad_norm(gl, 1.0, result, ws)
+    torch.cuda.synchronize()
+    assert float(result[0]) == pytest.approx(840 ** 0.5, rel=1e-6)
