@@ -569,35 +569,37 @@ static void grad_launches(uint32_t count, const GradTensorDev* list, float max_n
 {
     Table tab;
     bool scaled = !clip;
-    {
-        ProfScope prof(kKGradNorm, s);
-        uint32_t at = 0;
-        do {
-            const uint64_t units = fill_table(tab, list + at, count - at);
-            const uint32_t blocks = cut_sums(tab, units);
-            const GradEnd end{ws, result, result + 2 + at, max_norm, at == 0, at + tab.count == count};
-            const dim3 grid(blocks ? blocks : 1), block(kGradBlock);
-            if (blocks && blocks <= kInlineSlots && units <= kGradBlocks && clip && end.first_table && end.last_table) {      // a workgroup per unit
-                hipLaunchKernelGGL((k_grad_squares<false, Table>), grid, block, 0, s, end, tab);
-                hipLaunchKernelGGL((k_grad_scale<true, Table>), grid, block, 0, s, end, tab);
-                scaled = true;
-            } else if (blocks <= kAloneSlots) {
-                hipLaunchKernelGGL((k_grad_squares<true, Table>), grid, block, 0, s, end, tab);
-            } else {
-                hipLaunchKernelGGL((k_grad_squares<false, Table>), grid, block, 0, s, end, tab);
-                hipLaunchKernelGGL(k_grad_finish<Table>, dim3(1), dim3(1024), 0, s, end, tab);
-            }
-            at += tab.count;
-        } while (at < count);
-    }
-    if (!scaled) {
-        ProfScope prof(kKGradScale, s);
-        for (uint32_t at = 0; at < count; at += tab.count) {
-            const uint64_t units = fill_table(tab, list + at, count - at);
-            const uint32_t blocks = cut_runs(tab, units, scale_run);
-            const GradEnd end{ws, result, result + 2 + at, max_norm, 0, 0};
-            if (blocks) hipLaunchKernelGGL((k_grad_scale<false, Table>), dim3(blocks), dim3(kGradBlock), 0, s, end, tab);
+    uint32_t at = 0;
+    do {
+        const uint64_t units = fill_table(tab, list + at, count - at);
+        const uint32_t blocks = cut_sums(tab, units);
+        const GradEnd end{ws, result, result + 2 + at, max_norm, at == 0, at + tab.count == count};
+        const dim3 grid(blocks ? blocks : 1), block(kGradBlock);
+        const bool alone = blocks <= kAloneSlots;
+        const bool inlined = blocks && blocks <= kInlineSlots && units <= kGradBlocks && clip && end.first_table && end.last_table;      // a workgroup per unit
+        {
+            ProfScope prof(kKGradNorm, s);
+            if (alone && !inlined) hipLaunchKernelGGL((k_grad_squares<true, Table>), grid, block, 0, s, end, tab);
+            else hipLaunchKernelGGL((k_grad_squares<false, Table>), grid, block, 0, s, end, tab);
         }
+        if (inlined) {
+            ProfScope prof(kKGradScale, s);
+            hipLaunchKernelGGL((k_grad_scale<true, Table>), grid, block, 0, s, end, tab);
+            scaled = true;
+        } else if (!alone) {
+            ProfScope prof(kKGradFinish, s);
+            hipLaunchKernelGGL(k_grad_finish<Table>, dim3(1), dim3(1024), 0, s, end, tab);
+        }
+        at += tab.count;
+    } while (at < count);
+    if (scaled) return;
+    for (at = 0; at < count; at += tab.count) {
+        const uint64_t units = fill_table(tab, list + at, count - at);
+        const uint32_t blocks = cut_runs(tab, units, scale_run);
+        if (blocks == 0) continue;
+        const GradEnd end{ws, result, result + 2 + at, max_norm, 0, 0};
+        ProfScope prof(kKGradScale, s);
+        hipLaunchKernelGGL((k_grad_scale<false, Table>), dim3(blocks), dim3(kGradBlock), 0, s, end, tab);
     }
 }
 
@@ -622,13 +624,14 @@ static void adam_launches(uint32_t count, const AdamTensorDev* list, const AdamD
             units += tab.t[i].units = units_of(tab.t[i]);
         }
         const uint32_t blocks = cut_runs(tab, units, [](const AdamTensorDev&) { return 1u; });
-        if (blocks) hipLaunchKernelGGL(k_adam_list<Table>, dim3(blocks), dim3(kGradBlock), 0, s, tab, result);
+        if (blocks == 0) continue;
+        ProfScope prof(kKAdamList, s);
+        hipLaunchKernelGGL(k_adam_list<Table>, dim3(blocks), dim3(kGradBlock), 0, s, tab, result);
     }
 }
 
 hipError_t launch_adam_list(int count, const AdamTensorDev* list, const AdamDev& adam, const float* result, hipStream_t s)
 {
-    ProfScope prof(kKAdamList, s);
     if ((uint32_t)count <= kShortTable) adam_launches<AdamTable<kShortTable>>(count, list, adam, result, s);
     else adam_launches<AdamTable<kAdamTableTensors>>(count, list, adam, result, s);
     return hipGetLastError();

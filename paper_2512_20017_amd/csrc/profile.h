@@ -8,7 +8,7 @@ namespace pbdr {
 enum KernelId {
     kKPreprocess = 0, kKCountVisible, kKTileCount, kKTileLists, kKPack, kKFill,
     kKCompositeFwd, kKCompositeBwd, kKPreprocessBwd, kKStats, kKGather, kKGroupCull, kKLoss, kKAdam, kKTileDepthSort,
-    kKGradNorm, kKGradScale, kKAdamList, kKernelCount
+    kKGradNorm, kKGradScale, kKAdamList, kKGradFinish, kKernelCount
 };
 
 struct ProfState {

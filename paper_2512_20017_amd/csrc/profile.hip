@@ -9,7 +9,7 @@ ProfState g_prof;
 
 static const char* const kKernelNames[kKernelCount] = {
     "k_preprocess", "k_count_visible", "k_tile_count", "k_tile_lists", "k_pack", "fill", "k_composite_fwd", "k_composite_bwd", "k_preprocess_bwd", "k_render_stats", "k_gather_splat_grads", "k_group_cull", "k_l1_loss", "k_adam_selective",
-    "k_tile_depth_sort", "k_grad_squares", "k_grad_scale", "k_adam_list"};
+    "k_tile_depth_sort", "k_grad_squares", "k_grad_scale", "k_adam_list", "k_grad_finish"};
 
 static void release()
 {

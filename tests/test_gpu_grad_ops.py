@@ -525,3 +525,36 @@ def test_a_list_that_was_refused_serves_tensors_that_came_back():
     B.pbdr_grad_norm(gl, 1.0, result, ws)
     torch.cuda.synchronize()
     assert float(result[0]) == pytest.approx(840 ** 0.5, rel=1e-6)
+
+
+@pytest.mark.parametrize("spec,op,want", [
+    ([((3, 900), F32, 0.5)], "norm", dict(k_grad_squares=1)),
+    ([((3, 900), F32, 0.5)], "clip", dict(k_grad_squares=1, k_grad_scale=1)),
+    ([((14, 90_000), F32, None)], "norm", dict(k_grad_squares=1, k_grad_finish=1)),
+    ([((14, 90_000), F32, None)], "clip", dict(k_grad_squares=1, k_grad_scale=1)),
+    ([((48, 60_001), F32, None)], "clip", dict(k_grad_squares=1, k_grad_finish=1, k_grad_scale=1)),
+    ([((100,), F32, None)] * 89, "norm", dict(k_grad_squares=2)),
+    ([((100,), F32, None)] * 89, "clip", dict(k_grad_squares=2, k_grad_scale=2)),
+    ([((100,), F32, None)] * 49, "adam", dict(k_adam_list=2)),
+    ([((3, 0), F32, None)], "clip", dict(k_grad_squares=1)),
+    ([((3, 0), F32, None)], "adam", dict()),
+], ids=lambda x: x if isinstance(x, str) else None)
+def test_each_launch_is_timed_under_its_kernel(spec, op, want):
+    ts, ms = make(spec, 3)
+    result, ws = torch.empty(2 + len(ts), device="cuda"), B.alloc_grad_workspace(len(ts))
+    gl = B.GradList(ts, visible=ms, out=[torch.empty_like(t) for t in ts])
+    al = B.AdamList(*[[t.clone() for t in ts] for _ in range(4)], [1e-3] * len(ts), visible=ms)
+    names = B.profile_kernel_names()
+    torch.cuda.synchronize()
+    B.pbdr_profile_begin((1 << len(names)) - 1, 16)
+    try:
+        if op == "adam":
+            B.pbdr_adam_selective_list(al, 0.9, 0.999, 1e-8, 1)
+        else:
+            (B.pbdr_grad_norm if op == "norm" else B.pbdr_grad_clip)(gl, 0.5, result, ws)
+        torch.cuda.synchronize()
+        got = {name: B.pbdr_profile_collect(k) for k, name in enumerate(names)}
+    finally:
+        B.pbdr_profile_end()
+    assert {name: count for name, (ms_, count) in got.items() if count} == want
+    assert all(ms_ > 0 for ms_, count in got.values() if count)
