@@ -558,3 +558,115 @@ def test_each_launch_is_timed_under_its_kernel(spec, op, want):
         B.pbdr_profile_end()
     assert {name: count for name, (ms_, count) in got.items() if count} == want
     assert all(ms_ > 0 for ms_, count in got.values() if count)
+
+
+# ------------------------------------------------------------------------------------------------------------ sizes and ranges at the ends
+@pytest.mark.parametrize("dtype,size", [(F32, 1e-39), (BF16, 1e-38), (F16, 1e-6)])
+def test_clipped_values_below_the_normal_numbers(dtype, size):
+    """Gradients around the smallest normal number of their type, a quarter of which is left: most of what is written is subnormal."""
+    ts, ms = make([((3, 1001), dtype, 0.5), ((5003,), dtype, None)], 21, size)
+    norm = reference(ts, ms, np.inf)[0]
+    run_clip(ts, ms, float(np.float32(norm * 0.25)))
+    x = ts[1].cpu().double() * 0.25
+    assert 0 < float(x.abs().median()) < float(torch.finfo(dtype).tiny)
+
+
+def test_launches_whose_workgroups_take_several_units_each():
+    """More units than a launch has workgroups (2^23): rows of one point, 2^24 - 1 of them, three times that for scaling."""
+    planes = (1 << 24) - 1
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    gs = [torch.randn(planes, 1, device="cuda", generator=gen) for _ in range(3)]
+    seen = torch.ones(1, dtype=torch.uint8, device="cuda")
+    outs = [torch.full_like(g, float("nan")) for g in gs]
+    result, ws = torch.empty(5, device="cuda"), B.alloc_grad_workspace(3)
+    B.pbdr_grad_clip(B.GradList(gs, visible=seen, out=outs), 100.0, result, ws)
+    torch.cuda.synchronize()
+    each = [float(g.double().norm()) for g in gs]
+    norm = float(np.sqrt(sum(e * e for e in each)))
+    # one lane of a workgroup adds all its terms here: 2^23 units / 2048 workgroups * 4 planes * 1.5 = 24,576 terms, 2^-53 each, and
+    # the root halves it: 1.4e-12 beside the rounding to fp32
+    for got, want in zip(result.tolist(), [norm, 100.0 / norm] + each):
+        assert abs(got - want) <= (EPS + 3e-12) * want
+    assert 0 < float(result[1]) < 1
+    for g, o in zip(gs, outs):
+        assert torch.equal(o, g * result[1])
+    p, m, v = torch.randn(planes, 1, device="cuda", generator=gen), outs[1], outs[2].square_()
+    q, g, a, b = (x.clone().view(1, planes) for x in (p, gs[0], m, v))
+    B.pbdr_adam_selective_list(B.AdamList([p], [gs[0]], [m], [v], [1e-2], visible=seen), 0.9, 0.999, 1e-15, 3, zero_grad=True)
+    B.pbdr_adam_selective(q, g, a, b, torch.ones(planes, dtype=torch.uint8, device="cuda"), 1e-2, 0.9, 0.999, 1e-15, 3, zero_grad=True)
+    torch.cuda.synchronize()
+    for got, want in ((p, q), (m, a), (v, b), (gs[0], g)):
+        assert torch.equal(got.view(-1), want.view(-1))
+    assert not gs[0].any()
+
+
+def test_adam_beyond_32_bits():
+    """Five rows of 2^30 + 3 entries with three used points, then the same memory as one row of all entries."""
+    n, planes = (1 << 30) + 3, 5
+    spots = [0, 777_777_777, n - 1]
+    p, m, v = (torch.zeros(planes, n, device="cuda") for _ in range(3))
+    g = torch.full((planes, n), float("nan"), device="cuda")
+    seen = torch.zeros(n, dtype=torch.uint8, device="cuda")
+    new = torch.arange(1.0, 16.0, device="cuda").view(planes, 3)
+    for k, at in enumerate(spots):
+        seen[at] = 1
+        g[:, at] = new[:, k]
+
+    def check():
+        for got, want in zip((p, m, v), small()):
+            assert torch.equal(torch.stack([got[:, at] for at in spots], 1), want)
+            assert all(int(torch.count_nonzero(row)) == 3 for row in got)
+
+    def small():      # pbdr_adam_selective on the used entries alone
+        q, h, a, b = torch.zeros(1, 15, device="cuda"), new.clone().view(1, 15), torch.zeros(1, 15, device="cuda"), torch.zeros(1, 15, device="cuda")
+        B.pbdr_adam_selective(q, h, a, b, torch.ones(15, dtype=torch.uint8, device="cuda"), 1e-2, 0.9, 0.999, 1e-8, 2)
+        return [x.view(planes, 3) for x in (q, a, b)]
+
+    B.pbdr_adam_selective_list(B.AdamList([p], [g], [m], [v], [1e-2], visible=seen), 0.9, 0.999, 1e-8, 2)
+    check()
+    for x in (p, m, v, g):
+        x.zero_()
+    for k, at in enumerate(spots):
+        g[:, at] = new[:, k]
+    flat = [x.view(-1) for x in (p, g, m, v)]
+    assert flat[0].numel() > 1 << 32
+    B.pbdr_adam_selective_list(B.AdamList(*[[x] for x in flat], [1e-2]), 0.9, 0.999, 1e-8, 2)
+    check()
+
+
+def test_clipping_and_updates_in_flight_on_several_streams():
+    """Each stream clips into buffers and updates parameters of its own, call upon call, nothing waiting between; all that is
+    written is compared with what the same calls leave one at a time."""
+    def work(name, spec):
+        ts, ms = make(spec, len(name))
+        adam = [k for k, t in enumerate(ts) if t.dtype == F32]
+
+        def one():
+            s = dict(out=[torch.zeros_like(t) for t in ts], result=torch.zeros(2 + len(ts), device="cuda"))
+            p, m, v = ([torch.zeros_like(ts[k]) for k in adam] for _ in range(3))
+            s["clip"] = B.GradList(ts, visible=ms, out=s["out"])
+            s["adam"] = B.AdamList(p, [ts[k] for k in adam], m, v, [1e-3] * len(adam), visible=[ms[k] for k in adam])
+            s["all"] = [s["result"], *s["out"], *p, *m, *v]
+            return s
+        return one
+
+    def run(s, ws, stream=None):
+        B.pbdr_grad_clip(s["clip"], 0.1, s["result"], ws, stream=stream)
+        B.pbdr_adam_selective_list(s["adam"], 0.9, 0.999, 1e-15, 2, clip=s["result"], stream=stream)
+
+    makers = [work(name, SPECS[name]) for name in ("odd rows", "more than a workgroup each", "a scene")]
+    spaces, streams = [B.alloc_grad_workspace(8) for _ in makers], [torch.cuda.Stream() for _ in makers]
+    want, states = [one() for one in makers], [[one() for _ in range(6)] for one in makers]
+    for s, ws in zip(want, spaces):
+        run(s, ws)
+        torch.cuda.synchronize()
+        assert 0 < float(s["result"][1]) < 1
+    for rep in range(6):
+        for row, ws, stream in zip(states, spaces, streams):
+            run(row[rep], ws, stream)
+    torch.cuda.synchronize()
+    for s, row in zip(want, states):
+        for got in row:
+            for a, b in zip(got["all"], s["all"]):
+                bits = torch.int32 if a.dtype == F32 else torch.int16
+                assert torch.equal(a.view(bits), b.view(bits))
