@@ -424,7 +424,10 @@ int pbdr_preprocess_bwd_batch_adam(const pbdr_scene* scene, int32_t num_views, c
  * pointers. A tensor is [planes][n] without gaps; n or planes may be 0 (its pointers are then not looked at). An entry is
  * USED if visible is NULL or visible[i] != 0 for its point i; entries that are not used are not counted, whatever they
  * hold, and keep their bits (one between used ones may be read and written back). Gradients of other learned things may
- * be in the same list (planes = 1, visible = NULL), in 16 bits too.
+ * be in the same list (planes = 1, visible = NULL), in 16 bits too: the norm counts them. pbdr_adam_selective_list updates
+ * 32-bit tensors only; who updates the others takes their gradients times result[1] (zero where that is 0), or lets
+ * pbdr_grad_clip write the whole list. A norm has to be complete before the first update, so a clipped step cannot use
+ * pbdr_preprocess_bwd_batch_adam, which updates as it goes.
  *
  * pbdr_grad_norm writes result (device, float [2 + num_tensors]):
  *   result[0]     = norm  = sqrt(sum of g^2 over the used entries of all tensors)

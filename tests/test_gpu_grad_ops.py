@@ -670,3 +670,31 @@ def test_clipping_and_updates_in_flight_on_several_streams():
             for a, b in zip(got["all"], s["all"]):
                 bits = torch.int32 if a.dtype == F32 else torch.int16
                 assert torch.equal(a.view(bits), b.view(bits))
+
+
+@pytest.mark.parametrize("bad", [None, float("nan"), float("inf")])
+def test_a_step_with_other_gradients_in_the_list(bad):
+    """Norm over a scene and 16-bit extras, Adam on the scene, the extras times the factor by torch: bit for bit what clipping the
+    whole list and pbdr_adam_selective leave, a gradient that is not finite among the extras too."""
+    spec = GAUSS + [((64, 33), BF16, None), ((63,), F16, None), ((17,), F32, None)]
+    ts, ms = make(spec, 12)
+    if bad is not None:
+        ts[-2][5] = bad
+    rng = np.random.default_rng(2)
+    p, m, v = ([torch.from_numpy(f(size=t.shape).astype(np.float32)).cuda() for t in ts[:5]] for f in (rng.normal, rng.normal, rng.uniform))
+    one, two = ([[x.clone() for x in xs] for xs in (ts, p, m, v)] for _ in range(2))
+    result, ws = torch.empty(2 + len(ts), device="cuda"), B.alloc_grad_workspace(len(ts))
+    grads, net_grads = one[0][:5], one[0][5:]
+    B.pbdr_grad_norm(B.GradList(grads + net_grads, visible=ms), 0.05, result, ws)
+    B.pbdr_adam_selective_list(B.AdamList(one[1], grads, one[2], one[3], [1e-3] * 5, visible=ms[:5]), 0.9, 0.999, 1e-8, 2, clip=result)
+    for g in net_grads:
+        g.copy_(torch.where(result[1] == 0, 0.0, g.float() * result[1]))
+    B.pbdr_grad_clip(B.GradList(two[0], visible=ms), 0.05, torch.empty_like(result), ws)
+    for k in range(5):
+        B.pbdr_adam_selective(two[1][k], two[0][k], two[2][k], two[3][k], ms[k], 1e-3, 0.9, 0.999, 1e-8, 2)
+    torch.cuda.synchronize()
+    assert float(result[1]) == 0.0 if bad is not None else 0 < float(result[1]) < 1
+    for a, b in zip(one[0][5:], two[0][5:]):
+        assert a.dtype == b.dtype and torch.equal(a, b) and bool(a.any()) == (bad is None)
+    for a, b in zip(one[1] + one[2] + one[3], two[1] + two[2] + two[3]):
+        assert torch.equal(a, b)
