@@ -427,9 +427,19 @@ def pbdr_adam_selective(param, grad, exp_avg, exp_avg_sq, visible, lr, beta1, be
 _GRAD_DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
-# All that the description of a tensor rests on. Each look is one map() over the list: 167 tensors take 37 us of the host's time (the
-# address alone 7), the 5 of a scene 1.7; the time goes by tensors and looks, one by one in a loop it is the same.
-_LOOKS = (torch.Tensor.data_ptr, torch.Tensor.shape.__get__, torch.Tensor.dtype.__get__, torch.Tensor.is_contiguous, torch.Tensor.get_device)
+_look = None
+
+
+def _tensor_look(tensors: list) -> bytes:
+    """All that the description of a list's tensors rests on (csrc/tensor_look.cpp); raises if it has not been built."""
+    global _look
+    if _look is None:
+        try:
+            from ._tensor_look import look
+        except ImportError as e:
+            raise RuntimeError("_tensor_look.so does not load: build it with `python paper_2512_20017_amd/build.py`") from e
+        _look = look
+    return _look(tensors)
 
 
 class _TensorList:
@@ -454,11 +464,8 @@ class _TensorList:
     def __len__(self):
         return len(self._columns[0])
 
-    def _look(self):
-        return [list(map(look, self._all)) for look in _LOOKS]
-
     def _describe(self):
-        seen = self._look()
+        seen = _tensor_look(self._all)
         device = self._all[0].device if self._all else None
         for t in self._all:
             if t.device != device:
@@ -482,7 +489,7 @@ class _TensorList:
         self.device, self._array, self._seen = device, self._structs(sizes), seen
 
     def array(self):
-        if self._look() != self._seen:
+        if _tensor_look(self._all) != self._seen:
             self._describe()
         return self._array
 

@@ -1,12 +1,15 @@
-"""Compile the HIP sources in csrc/ into paper_2512_20017_amd/libpbdr.so for gfx950 (cross-compiles without a GPU)."""
+"""Compile the HIP sources in csrc/ into paper_2512_20017_amd/libpbdr.so for gfx950 (cross-compiles without a GPU), and the binding's
+host helper csrc/tensor_look.cpp into paper_2512_20017_amd/_tensor_look.so."""
 import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpbdr.so")
+LOOK = os.path.join(HERE, "_tensor_look.so")
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-munsafe-fp-atomics",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-function"]
@@ -21,7 +24,21 @@ def build(verbose: bool = False, extra=()) -> str:
     if verbose:
         print(" ".join(cmd))
     subprocess.run(cmd, check=True)
+    build_look(verbose)
     return LIB
+
+
+def build_look(verbose: bool = False) -> str:
+    """The binding's look at lists of tensors: host C++ against PyTorch's headers, a Python module of its own."""
+    import torch
+    from torch.utils.cpp_extension import include_paths
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+           f"-I{sysconfig.get_path('include')}", *[f"-isystem{p}" for p in include_paths()], "-o", LOOK, os.path.join(CSRC, "tensor_look.cpp"),
+           "-L" + os.path.join(os.path.dirname(torch.__file__), "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"]
+    if verbose:
+        print(" ".join(cmd))
+    subprocess.run(cmd, check=True)
+    return LOOK
 
 
 def build_ubench(verbose: bool = False) -> str:

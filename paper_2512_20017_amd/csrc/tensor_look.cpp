@@ -1,0 +1,50 @@
+// What a list of tensors of the binding rests on, in one call: a bytes object of the address, type, device, order and shape of every
+// tensor of a Python list. Two looks differ if a tensor has come to lie elsewhere or in another form. (Order: in rows without gaps
+// or not; lists take no tensor that is not.) 167 tensors take 1.1 us of the host's time; asked one by one from Python they take 37,
+// more than the calls themselves. Host code only, a module of its own: libpbdr.so knows nothing of PyTorch.
+#include <Python.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <exception>
+
+static PyObject* look(PyObject*, PyObject* list)
+{
+    if (!PyList_Check(list)) {
+        PyErr_SetString(PyExc_TypeError, "pbdr: not a list of tensors");
+        return nullptr;
+    }
+    const Py_ssize_t count = PyList_GET_SIZE(list);
+    PyObject* out = nullptr;
+    try {
+        Py_ssize_t words = 0;
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            PyObject* o = PyList_GET_ITEM(list, i);
+            if (!THPVariable_Check(o)) {
+                PyErr_Format(PyExc_TypeError, "pbdr: %R is no tensor", o);
+                return nullptr;
+            }
+            words += 3 + (Py_ssize_t)THPVariable_Unpack(o).dim();
+        }
+        out = PyBytes_FromStringAndSize(nullptr, words * (Py_ssize_t)sizeof(int64_t));
+        if (out == nullptr) return nullptr;
+        int64_t* w = reinterpret_cast<int64_t*>(PyBytes_AS_STRING(out));
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            const at::Tensor& t = THPVariable_Unpack(PyList_GET_ITEM(list, i));
+            const c10::Device d = t.device();
+            *w++ = static_cast<int64_t>(reinterpret_cast<intptr_t>(t.const_data_ptr()));
+            *w++ = static_cast<int64_t>(t.scalar_type()) | static_cast<int64_t>(static_cast<uint8_t>(d.type())) << 8 |
+                   static_cast<int64_t>(static_cast<uint8_t>(d.index())) << 16 | static_cast<int64_t>(t.is_contiguous()) << 24;
+            *w++ = t.dim();
+            for (const int64_t s : t.sizes()) *w++ = s;
+        }
+        return out;
+    } catch (const std::exception& e) {      // a tensor without memory or without plain sizes
+        Py_XDECREF(out);
+        PyErr_Format(PyExc_ValueError, "pbdr: %s", e.what());
+        return nullptr;
+    }
+}
+
+static PyMethodDef methods[] = {{"look", look, METH_O, "look(list of tensors) -> bytes"}, {nullptr, nullptr, 0, nullptr}};
+static PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensor_look", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+PyMODINIT_FUNC PyInit__tensor_look(void) { return PyModule_Create(&module); }

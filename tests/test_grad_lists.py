@@ -252,3 +252,16 @@ def test_a_list_does_not_keep_memory_that_its_tensors_have_left():
     assert left() is not None
     t.data = torch.zeros(3, 8)
     assert left() is None and len(lists) == 3
+
+
+def test_what_is_looked_at():
+    t = torch.zeros(1000)[:24].view(4, 6)
+    look = lambda x: B._tensor_look([x])      # noqa: E731
+    others = [t.view(6, 4), t.view(24), t.view(1, 4, 6), t[:2], t[:, :5], t.t(), t.view(-1)[1:].view(23), t.view(torch.int32), torch.zeros(4, 6)]
+    seen = [look(x) for x in others]
+    assert look(t) == look(t.view(4, 6)) and look(t) not in seen and len(set(seen)) == len(seen)
+    assert look(t.view(-1)[:12].view(torch.float16)) != look(t.view(-1)[:12].view(torch.bfloat16))
+    assert B._tensor_look([]) == b"" and B._tensor_look([t, others[0]]) != B._tensor_look([others[0], t])
+    for bad in (t, (t,), [t, None], [np.zeros(3)]):
+        with pytest.raises(TypeError):
+            B._tensor_look(bad)
