@@ -596,7 +596,7 @@ def pbdr_grad_clip(grads: GradList, max_norm: float, result: torch.Tensor, ws: t
 
 
 def pbdr_adam_selective_list(adam: AdamList, beta1, beta2, eps, step, clip: torch.Tensor = None, zero_grad=False, stream=None) -> None:
-    """pbdr_adam_selective on every tensor of the list in one launch; clip: the result of pbdr_grad_norm, whose factor the
+    """pbdr_adam_selective on every tensor of the list, 48 tensors a launch; clip: the result of pbdr_grad_norm, whose factor the
     gradients are taken times, None: as they are."""
     array = adam.array()
     if len(array) == 0:

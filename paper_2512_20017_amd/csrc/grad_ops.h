@@ -12,11 +12,20 @@ constexpr int kDenseVecs = 2;
 // Planes of a masked unit that sums or scales, all of which are read before the first is used (8M points, a quarter used: norm 97 us;
 // 2 planes 136, 3 planes 97, 8 planes 100, where scaling runs out of registers).
 constexpr uint32_t kMaskPlanes = 4;
-// A workgroup that finds nothing to do still costs half a nanosecond of the launch, and large scenes are seen in small part: from
-// kManyPoints on a workgroup scales kScaleRun units (8M points clipped: 5 % used 174 -> 130 us, 25 % used 377 and 379) and Adam takes
-// eight planes a unit instead of two (5 % used 319 -> 223, 10 % 382 -> 339, 25 % 738 -> 748). Below, workgroups have to be many
-// enough to fill the chip evenly: four planes (1.5M points, 5 % used 69 -> 60 us; 8 planes 54, but 1M points, 60 % used, 212 instead of
-// 208), and one below kFewPoints (200,003 surfels, 70 % used: 54 us; 2 planes 56, 4 planes 58, 8 planes 61).
+// A workgroup that finds nothing to do still costs half a nanosecond of the launch, and large scenes are seen in small part: many planes
+// a unit pay where little is used, few where much is, since workgroups then end more evenly. The used share is not known on the
+// host, so the number of points decides, where the gain of the one has come to outweigh the loss of the other. Norm and Adam, SH3, us:
+//   points      5 % used, 1 / 4 / 8 planes     25 % used              60 % used
+//   200,000       24 /  21 /  25                30 /  31 /  35         48 /  50 /  54
+//   300,000       31 /  24 /  29                40 /  39 /  43         69 /  71 /  73
+//   600,000       51 /  33 /  36                69 /  66 /  67        129 / 132 / 130
+//   1,500,000    111 /  59 /  54               154 / 141 / 143        301 / 311 / 317
+//   3,500,000      - / 118 / 102                 - / 320 / 323          - / 759 / 776
+//   4,500,000      - / 149 / 130                 - / 411 / 413          - / 999 / 999
+//   8,000,000      - / 253 / 217                 - / 735 / 748
+// Scaling takes runs of kScaleRun units of a masked tensor from kManyPoints on: clipped with runs of one and of four, 3.5M points 79
+// and 56 us at 5 %, 372 and 378 at 60 %; 4.5M points 99 and 72, 478 and 487; 8M points 172 and 131, 377 and 377 at 25 %. Smaller
+// scenes keep the form that is better for what a batch usually sees of them (1.5M points: 41 and 34, 157 and 161).
 constexpr uint64_t kFewPoints = 400000, kManyPoints = 4000000;
 constexpr uint32_t kScaleRun = 4;
 // Workgroups of a launch that sums, eight per compute unit: units that need no reading leave gaps in masked tensors (8M points, a

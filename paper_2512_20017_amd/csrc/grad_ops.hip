@@ -241,7 +241,8 @@ __global__ __launch_bounds__(1024) void k_grad_finish(GradEnd end, Table tab)
 }
 
 // Every workgroup sums its part into a slot. 1M points SH3 (236 MB): 39 us, 6.0 TB/s; 8M points of which a quarter is used (466 MB):
-// 94 us, 5.0 TB/s, and a tenth of the values' bytes in addition for the masks, which the last-level cache gives again for every unit.
+// 95 us, 4.9 TB/s; the counters say 574 MB, since each of a stretch's sixteen units asks for the mask (128 MB in all, part of it from the
+// caches) and runs of used points end inside lines.
 // Masks that come several units early, units of more planes and 4,096 workgroups made the latter 3 to 40 % slower.
 // kAlone: the last workgroup to be done finishes in the same launch: slots go past the caches of the eight dies (agent scope), and
 // the counter is left at zero for the next launch.
@@ -373,9 +374,10 @@ __device__ void write_scaled(const GradTensorDev& t, float scale, uint32_t begin
     }
 }
 
-// One unit per workgroup (2,048 workgroups that walk over the units took 4 to 10 % longer), four of a masked tensor of many points. 1M points SH3: 66 us for 236 MB read and
-// written, 7.2 TB/s: most of what is read is still in the last-level cache, since nothing else of the two passes goes there. 2M
-// surfels, twice what it holds: 148 us, 6.5 TB/s. kFinish: every workgroup adds the slots up for itself, one writes the result: for
+// One unit per workgroup (2,048 workgroups that walk over the units took 4 to 10 % longer), four of a masked tensor of many points.
+// 1M points SH3: 66 us for 236 MB read and written, 7.2 TB/s: most of what is read is still in the last-level cache, since nothing
+// else of the two passes goes there. 2M surfels, twice what it holds: 148 us, 6.5 TB/s. 8M points of which a quarter is used: 234 us
+// into another buffer, of which it reads the lines that are used in part, 0.32 GB, 178 us in place. kFinish: every workgroup adds the slots up for itself, one writes the result: for
 // small lists, whose sums then need no ending.
 template <bool kFinish, class Table>
 __global__ __launch_bounds__(kGradBlock, 8) void k_grad_scale(GradEnd end, Table tab)
@@ -391,9 +393,9 @@ __global__ __launch_bounds__(kGradBlock, 8) void k_grad_scale(GradEnd end, Table
     else write_scaled<kGradBF16>(t, scale, begin, stop);
 }
 
-// Adam, a unit per workgroup: 28 bytes an entry, and the gradient's four again. 1M points SH3, 60 % used: 173 us for 0.96 GB beside a
-// gradient that is still cached, 5.5 TB/s; 8M points, a quarter used: 648 us for 3.2 GB and 0.46 GB of gradient, 5.7 TB/s. With
-// ordinary loads and stores of parameters and moments 203 us at 1M points, forwards 680 us at 8M.
+// Adam, a unit per workgroup: 28 bytes an entry, the gradient's four among them (32 with zero_grad). 1M points SH3, 60 % used: 172 us for
+// 0.96 GB, 5.6 TB/s, part of the gradient from the last-level cache; 8M points, a quarter used: 647 us for 3.2 GB, 5.0 TB/s (3.46 GB and
+// 5.35 TB/s by the counters). With ordinary loads and stores of parameters and moments 203 us at 1M points, forwards 680 us at 8M.
 // A lane takes four entries of a row, and a workgroup's stretch of a row begins on a cache line of the moments, wherever the row
 // begins: lines that two wavefronts write in part cost 12 % of the whole (with the norm 200,003 surfels 64 us, 200,000 surfels 57). So
 // lanes may stand before the row's begin, and the mask is read at the plane's own offset. The vectors of parameter, gradient and
