@@ -31,7 +31,8 @@ static PyObject* look(PyObject*, PyObject* list)
         for (Py_ssize_t i = 0; i < count; ++i) {
             const at::Tensor& t = THPVariable_Unpack(PyList_GET_ITEM(list, i));
             const c10::Device d = t.device();
-            *w++ = static_cast<int64_t>(reinterpret_cast<intptr_t>(t.const_data_ptr()));
+            // memory of its own: what a tensor shares with a lazy copy until one of them is written is parted here
+            *w++ = static_cast<int64_t>(reinterpret_cast<intptr_t>(t.mutable_data_ptr()));
             *w++ = static_cast<int64_t>(t.scalar_type()) | static_cast<int64_t>(static_cast<uint8_t>(d.type())) << 8 |
                    static_cast<int64_t>(static_cast<uint8_t>(d.index())) << 16 | static_cast<int64_t>(t.is_contiguous()) << 24;
             *w++ = t.dim();

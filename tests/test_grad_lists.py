@@ -265,3 +265,12 @@ def test_what_is_looked_at():
     for bad in (t, (t,), [t, None], [np.zeros(3)]):
         with pytest.raises(TypeError):
             B._tensor_look(bad)
+
+
+def test_memory_shared_until_it_is_written_is_not_written():
+    t = torch.zeros(3, 8)
+    a = B.GradList([t])
+    a.array()
+    other = torch._lazy_clone(t)
+    at = a.array()[0].data
+    assert at == t.data_ptr() != other.data_ptr()
