@@ -377,8 +377,8 @@ __device__ void write_scaled(const GradTensorDev& t, float scale, uint32_t begin
 // One unit per workgroup (2,048 workgroups that walk over the units took 4 to 10 % longer), four of a masked tensor of many points.
 // 1M points SH3: 66 us for 236 MB read and written, 7.2 TB/s: most of what is read is still in the last-level cache, since nothing
 // else of the two passes goes there. 2M surfels, twice what it holds: 148 us, 6.5 TB/s. 8M points of which a quarter is used: 234 us
-// into another buffer, of which it reads the lines that are used in part, 0.32 GB, 178 us in place. kFinish: every workgroup adds the slots up for itself, one writes the result: for
-// small lists, whose sums then need no ending.
+// into another buffer, of which it reads the lines that are used in part, 0.32 GB, 178 us in place. kFinish: every workgroup adds the
+// slots up for itself, one writes the result: for small lists, whose sums then need no ending.
 template <bool kFinish, class Table>
 __global__ __launch_bounds__(kGradBlock, 8) void k_grad_scale(GradEnd end, Table tab)
 {
